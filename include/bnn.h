@@ -493,6 +493,91 @@ typedef enum {
 BNN_API size_t bnn_pipe_rate_scratch_bytes(int which);
 BNN_API int bnn_pipe_rate(int which, int repeat, void* scratch, size_t scratch_bytes, double* work, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * 4-bit floating point: layers between the binary and the real-valued ones (the paper has no
+ * counterpart; its Section 3.1 keeps the layers that suffer from one bit in fp32).
+ *
+ * An element is an e2m1 number (a sign and 0, .5, 1, 1.5, 2, 3, 4 or 6) times the scale of its block.
+ *   BNN_F4_E8M0_32 : blocks of 32 along K, scale 2^(byte - 127), byte 255 = NaN;
+ *   BNN_F4_E4M3_16 : blocks of 16 along K, scale an e4m3 number >= 0, byte 127 = NaN.
+ * Stored form of a matrix [rows][K]:
+ *   codes  : rows of bytes with a pitch that is a multiple of 16 and at least bnn_f4_pitch(K) =
+ *            16 * ceil(K/32), base 16-byte aligned; element k is the low (k even) or the high nibble
+ *            of byte k/2 (bit 3 the sign, bits 2-1 the exponent, bit 0 the mantissa).  Kernels that write a row
+ *            write all bnn_f4_pitch(K) bytes, with 0 behind K, and kernels that read it rely on these zeros.
+ *   scales : tiles of 512 bytes that hold 128 rows x 4 consecutive blocks, 16-byte aligned base,
+ *            [row tile][tile along K]; the byte of row r and block b OF A TILE is (r % 32) * 16 + (r / 32) * 4 + b.
+ *            Scales of blocks at or beyond K, up to the next multiple of four blocks, are 0.
+ *            bnn_f4_scale_bytes(format, rows, K, groups) bytes.
+ * Rows in groups (experts): offsets[0 .. groups] (DEVICE, ascending) -- group g has the rows
+ * offsets[g] .. offsets[g+1]-1, and row tiles of its own, from tile offsets[g] / 128 + g on; a matrix without
+ * offsets is one group.  Rows before the first and behind the last group are neither read nor written.  Offsets that
+ * do not ascend or leave the matrix give unspecified results, but no access outside the buffers.
+ * groups <= 1024, K <= 2^24. */
+typedef enum { BNN_F4_E8M0_32 = 0, BNN_F4_E4M3_16 = 1 } bnn_f4_format;
+typedef enum { BNN_DTYPE_F32 = 0, BNN_DTYPE_F16 = 1, BNN_DTYPE_BF16 = 2 } bnn_dtype;
+BNN_API int bnn_f4_pitch(int K);
+BNN_API size_t bnn_f4_scale_bytes(int format, int rows, int K, int groups);
+
+/* Quantisation.  Row r of the result is row source[r] of X (source NULL: row r; an index outside
+ * 0 .. src_rows-1 gives a row of zeros), times 2^exponent (|exponent| <= 64; e4m3 scales lose precision below 2^-6, which
+ * is where weights of a fan-in of some thousands lie).  Scale of a block with largest magnitude m:
+ *   E8M0_32 : 2^(floor(log2 m) - 2), at least 2^-127;   E4M3_16 : m / 6 to the nearest e4m3 number, at most 448;
+ * codes: x / scale to the nearest, ties to even, magnitudes above 6 become 6; zeros where the scale is 0.  A block with a NaN or an infinity
+ * gets the scale NaN.  X : [src_rows][ldx] of `dtype`.
+ * Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN (codes, scales, pitch; X to its element), BNN_ERR_UNSUPPORTED (unknown
+ * format or type), BNN_ERR_WORKSPACE (scale_bytes too small). */
+BNN_API int bnn_f4_quantize(const void* X, int dtype, int src_rows, int K, int ldx, const int32_t* source,
+                    const int32_t* offsets, int groups, int rows, int format, int exponent,
+                    void* codes, int ldc, void* scales, size_t scale_bytes, void* stream);
+
+/* The values that a quantised matrix stands for, times 2^exponent, rounded once to `dtype`.  Y : [rows][ldy].
+ * Errors as bnn_f4_quantize. */
+BNN_API int bnn_f4_dequantize(const void* codes, int ldc, const void* scales, size_t scale_bytes,
+                      const int32_t* offsets, int groups, int rows, int K, int format, int exponent,
+                      void* Y, int dtype, int ldy, void* stream);
+
+/* Product of two quantised matrices of one format, Eq. 1 with 4-bit weights and inputs:
+ *   Y[m][n] = act(fma(scale[n], 2^exponent * sum_k a[m][k] w[n][k], shift[n]))
+ * with fp32 sums.  A : [M] rows, W : [N] rows in the stored form above.  epi (may be NULL): scale, shift, and act
+ * BNN_ACT_NONE / HARDTANH / SIGMOID with Y [M][ldy] of `dtype`, or BNN_ACT_SIGN_PACK with Y NULL and out_bits (the input of a
+ * binary layer).  Any M from one row on.
+ * bnn_f4_gemm_grouped: group g's rows of A by W's rows g * N .. g * N + N - 1; W is [groups * N] rows whose scales are stored with
+ * offsets[g] = g * N; scale and shift are [groups][N].
+ * Errors: as bnn_f4_quantize; BNN_ERR_UNSUPPORTED also for an act that is not named above. */
+BNN_API int bnn_f4_gemm(const void* A, int lda, const void* a_scales, size_t a_scale_bytes,
+                const void* W, int ldw, const void* w_scales, size_t w_scale_bytes,
+                int M, int N, int K, int format, int exponent, void* Y, int dtype, int ldy,
+                const bnn_epilogue* epi, void* stream);
+BNN_API int bnn_f4_gemm_grouped(const void* A, int lda, const void* a_scales, size_t a_scale_bytes,
+                        const int32_t* offsets, int groups,
+                        const void* W, int ldw, const void* w_scales, size_t w_scale_bytes,
+                        int M, int N, int K, int format, int exponent, void* Y, int dtype, int ldy,
+                        const bnn_epilogue* epi, void* stream);
+
+/* Router of a layer that is split into E experts (the paper has no counterpart).  logits : [T][ld] of
+ * `dtype`.  For each token t, the k experts with the largest logits, descending, ties to the lowest expert:
+ *   index [T][k]  : the experts;   weight [T][k] : fp32, softmax over all E logits (BNN_ROUTE_SOFTMAX) or over the chosen ones
+ *                   (BNN_ROUTE_SOFTMAX_CHOSEN);
+ * and the (token, choice) pairs sorted by expert, by token within an expert:
+ *   offsets [E+1] : where each expert's pairs begin;   slot [T][k] : a pair's place;
+ *   source [T*k]  : the token of the pair at a place -- what bnn_f4_quantize takes as `source`.
+ * An expert with the logit -inf (or NaN) is not chosen.  Where fewer than k are left, index and slot are -1 and the
+ * weight 0; places from offsets[E] on are not written.  A NaN makes all of its token's weights NaN, and so does +inf.
+ * E <= 1024, k <= 32, k <= E.  workspace: bnn_route_workspace_bytes(T, E) bytes, not used after the call's work is done.
+ * Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN, BNN_ERR_UNSUPPORTED, BNN_ERR_WORKSPACE. */
+typedef enum { BNN_ROUTE_SOFTMAX = 0, BNN_ROUTE_SOFTMAX_CHOSEN = 1 } bnn_route_mode;
+BNN_API size_t bnn_route_workspace_bytes(int T, int E);
+BNN_API int bnn_route_experts(const void* logits, int dtype, int T, int E, int ld, int k, int mode,
+                      int32_t* index, float* weight, int32_t* offsets, int32_t* slot, int32_t* source,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* The experts' results brought back to their tokens: Y[t] = sum_j weight[t][j] * Z[slot[t][j]], fp32 sums in the
+ * order of j.  Z : [rows][ldz], slot and weight : [T][k], Y : [T][ldy].  A slot outside 0 .. rows-1 adds nothing (whatever its weight).
+ * Y may not overlap Z.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN (to the element), BNN_ERR_UNSUPPORTED. */
+BNN_API int bnn_combine_experts(const void* Z, int z_dtype, int rows, int ldz, const int32_t* slot, const float* weight,
+                        int T, int k, int N, void* Y, int y_dtype, int ldy, void* stream);
+
 /* Smallest legal packed pitch (in words) for rows of K bits: ceil(K/32) rounded up to 4. */
 BNN_API int bnn_packed_pitch(int K);
 

@@ -131,6 +131,25 @@ def lib():
         L.bnn_forward_static.restype = C.c_int
         L.bnn_forward_events.argtypes = [C.POINTER(Model), p, i, i, p, i, p, C.c_size_t, C.POINTER(p),
                                          C.POINTER(p), p]
+        z = C.c_size_t
+        L.bnn_f4_pitch.argtypes = [i]
+        L.bnn_f4_pitch.restype = i
+        L.bnn_f4_scale_bytes.argtypes = [i, i, i, i]
+        L.bnn_f4_scale_bytes.restype = z
+        L.bnn_f4_quantize.argtypes = [p, i, i, i, i, p, p, i, i, i, i, p, i, p, z, p]
+        L.bnn_f4_quantize.restype = i
+        L.bnn_f4_dequantize.argtypes = [p, i, p, z, p, i, i, i, i, i, p, i, i, p]
+        L.bnn_f4_dequantize.restype = i
+        L.bnn_f4_gemm.argtypes = [p, i, p, z, p, i, p, z, i, i, i, i, i, p, i, i, C.POINTER(Epilogue), p]
+        L.bnn_f4_gemm.restype = i
+        L.bnn_f4_gemm_grouped.argtypes = [p, i, p, z, p, i, p, i, p, z, i, i, i, i, i, p, i, i, C.POINTER(Epilogue), p]
+        L.bnn_f4_gemm_grouped.restype = i
+        L.bnn_route_workspace_bytes.argtypes = [i, i]
+        L.bnn_route_workspace_bytes.restype = z
+        L.bnn_route_experts.argtypes = [p, i, i, i, i, i, i, p, p, p, p, p, p, z, p]
+        L.bnn_route_experts.restype = i
+        L.bnn_combine_experts.argtypes = [p, i, i, i, p, p, i, i, i, p, i, i, p]
+        L.bnn_combine_experts.restype = i
         for name in ("bnn_pack_weights", "bnn_binarize_pack", "bnn_fold_thresholds", "bnn_xnor_gemm",
                      "bnn_signw_gemm", "bnn_output_layer", "bnn_forward", "bnn_forward_events"):
             getattr(L, name).restype = C.c_int
@@ -475,3 +494,151 @@ def bnn_forward_static(model: ModelDesc, X, logp):
     _check(lib().bnn_forward_static(C.byref(model.c), _ptr(X, torch.float32), _ld(X), X.shape[0],
                                     _ptr(logp, torch.float32), _ld(logp), _stream()), "bnn_forward_static")
     return logp
+
+
+# ---- 4-bit floating point and experts ----
+F4_E8M0_32, F4_E4M3_16 = 0, 1
+ROUTE_SOFTMAX, ROUTE_SOFTMAX_CHOSEN = 0, 1
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _dtype(t):
+    if t.dtype not in _DTYPES:
+        raise TypeError("expected float32, float16 or bfloat16, got %s" % t.dtype)
+    return _DTYPES[t.dtype]
+
+
+def _here(*tensors):
+    """All tensors given lie on the device that the call runs on."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError("expected a tensor on the current CUDA device %d, got one on %s" % (dev, t.device))
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _flat(t, dtype, n, what):
+    """Address of a contiguous tensor of exactly n elements."""
+    if t.dtype != dtype:
+        raise TypeError("%s: expected dtype %s, got %s" % (what, dtype, t.dtype))
+    _need(t.numel() == n and t.is_contiguous(), "%s: expected %d contiguous elements" % (what, n))
+    return t.data_ptr()
+
+
+def bnn_f4_pitch(K) -> int:
+    """Bytes of a row of codes."""
+    return int(lib().bnn_f4_pitch(int(K)))
+
+
+def bnn_f4_scale_bytes(fmt, rows, K, groups=1) -> int:
+    return int(lib().bnn_f4_scale_bytes(int(fmt), int(rows), int(K), int(groups)))
+
+
+def _groups(offsets):
+    """(address, number of groups)"""
+    if offsets is None:
+        return None, 1
+    return _flat(offsets, torch.int32, offsets.numel(), "offsets"), offsets.numel() - 1
+
+
+def _scales(t):
+    """(address, bytes)"""
+    return _flat(t, torch.uint8, t.numel(), "scales"), t.numel()
+
+
+def bnn_f4_quantize(X, codes, scales, fmt=F4_E8M0_32, source=None, offsets=None, exponent=0):
+    """Rows of X (gathered by ``source``) -> ``codes`` (uint8 [rows][pitch]) and ``scales`` (uint8, bnn_f4_scale_bytes)."""
+    _here(X, codes, scales, source, offsets)
+    rows = codes.shape[0]
+    off, groups = _groups(offsets)
+    sc, sb = _scales(scales)
+    src = None if source is None else _flat(source, torch.int32, rows, "source")
+    _check(lib().bnn_f4_quantize(X.data_ptr(), _dtype(X), X.shape[0], X.shape[1], _ld(X), src, off, groups, rows, fmt, exponent,
+                                 _ptr(codes, torch.uint8), _ld(codes), sc, sb, _stream()), "bnn_f4_quantize")
+    return codes, scales
+
+
+def bnn_f4_dequantize(codes, scales, Y, fmt=F4_E8M0_32, offsets=None, exponent=0):
+    """The values of a quantised matrix, in Y's type."""
+    _here(codes, scales, Y, offsets)
+    _need(codes.shape[0] == Y.shape[0], "codes and Y have different numbers of rows")
+    off, groups = _groups(offsets)
+    sc, sb = _scales(scales)
+    _check(lib().bnn_f4_dequantize(_ptr(codes, torch.uint8), _ld(codes), sc, sb, off, groups, Y.shape[0], Y.shape[1], fmt, exponent,
+                                   Y.data_ptr(), _dtype(Y), _ld(Y), _stream()), "bnn_f4_dequantize")
+    return Y
+
+
+def _f4_output(rows, n, y, act, sign_mode, scale, shift, out_bits, per):
+    """(Y, dtype, ldy, epilogue)"""
+    for t in (scale, shift):
+        if t is not None:
+            _flat(t, torch.float32, per, "scale, shift")
+    if out_bits is not None:
+        _need(out_bits.shape[0] == rows, "out_bits has another number of rows")
+    epi = None
+    if act != ACT_NONE or scale is not None or shift is not None or out_bits is not None:
+        epi = C.byref(_epilogue(act, sign_mode, scale, shift, out_bits=out_bits))
+    if y is None:
+        return None, 0, 0, epi
+    _need(tuple(y.shape) == (rows, n), "Y: expected [%d, %d]" % (rows, n))
+    return y.data_ptr(), _dtype(y), _ld(y), epi
+
+
+def bnn_f4_gemm(A, a_scales, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0, act=ACT_NONE, scale=None, shift=None,
+                out_bits=None, sign_mode=SIGN_ZERO_POS):
+    """Y = act(fma(scale, 2^exponent * A W^T, shift)) of two quantised matrices (codes uint8 [rows][pitch], scales)."""
+    _here(A, a_scales, W, w_scales, Y, scale, shift, out_bits)
+    m, n = A.shape[0], W.shape[0]
+    (sa, ba), (sw, bw) = _scales(a_scales), _scales(w_scales)
+    y, dt, ldy, epi = _f4_output(m, n, Y, act, sign_mode, scale, shift, out_bits, n)
+    _check(lib().bnn_f4_gemm(_ptr(A, torch.uint8), _ld(A), sa, ba, _ptr(W, torch.uint8), _ld(W), sw, bw, m, n, K, fmt, exponent,
+                             y, dt, ldy, epi, _stream()), "bnn_f4_gemm")
+    return Y if out_bits is None else out_bits
+
+
+def bnn_f4_gemm_grouped(A, a_scales, offsets, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0, act=ACT_NONE, scale=None,
+                        shift=None, out_bits=None, sign_mode=SIGN_ZERO_POS):
+    """The same by groups of A's rows; ``W``: codes uint8 [groups][N][pitch], ``scale`` / ``shift``: [groups][N]."""
+    _here(A, a_scales, offsets, W, w_scales, Y, scale, shift, out_bits)
+    off, groups = _groups(offsets)
+    _need(W.dim() == 3 and W.shape[0] == groups and W.stride(2) == 1 and (groups == 1 or W.stride(0) == W.shape[1] * W.stride(1)),
+          "W: expected [%d, N, pitch], the groups one behind the other" % groups)
+    m, n = A.shape[0], W.shape[1]
+    (sa, ba), (sw, bw) = _scales(a_scales), _scales(w_scales)
+    y, dt, ldy, epi = _f4_output(m, n, Y, act, sign_mode, scale, shift, out_bits, groups * n)
+    _check(lib().bnn_f4_gemm_grouped(_ptr(A, torch.uint8), _ld(A), sa, ba, off, groups, _ptr(W, torch.uint8), W.stride(1), sw, bw,
+                                     m, n, K, fmt, exponent, y, dt, ldy, epi, _stream()), "bnn_f4_gemm_grouped")
+    return Y if out_bits is None else out_bits
+
+
+def bnn_route_workspace_bytes(T, E) -> int:
+    return int(lib().bnn_route_workspace_bytes(int(T), int(E)))
+
+
+def bnn_route_experts(logits, index, weight, offsets, slot, source, workspace, mode=ROUTE_SOFTMAX):
+    """The k best experts of each token, their weights, and the tokens sorted by expert (k = index.shape[1])."""
+    _here(logits, index, weight, offsets, slot, source, workspace)
+    (t, e), k = logits.shape, index.shape[1]
+    _need(index.shape[0] == t, "index has another number of tokens")
+    i32 = torch.int32
+    _check(lib().bnn_route_experts(logits.data_ptr(), _dtype(logits), t, e, _ld(logits), k, mode, _flat(index, i32, t * k, "index"),
+                                   _flat(weight, torch.float32, t * k, "weight"), _flat(offsets, i32, e + 1, "offsets"),
+                                   _flat(slot, i32, t * k, "slot"), _flat(source, i32, t * k, "source"), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream()), "bnn_route_experts")
+    return index, weight, offsets, slot, source
+
+
+def bnn_combine_experts(Z, slot, weight, Y):
+    """Y[t] = sum_j weight[t][j] * Z[slot[t][j]]."""
+    _here(Z, slot, weight, Y)
+    t, k = slot.shape
+    _need(Y.shape[0] == t and Y.shape[1] == Z.shape[1], "Y: expected [%d, %d]" % (t, Z.shape[1]))
+    _check(lib().bnn_combine_experts(Z.data_ptr(), _dtype(Z), Z.shape[0], _ld(Z), _flat(slot, torch.int32, t * k, "slot"),
+                                     _flat(weight, torch.float32, t * k, "weight"), t, k, Z.shape[1], Y.data_ptr(), _dtype(Y), _ld(Y),
+                                     _stream()), "bnn_combine_experts")
+    return Y

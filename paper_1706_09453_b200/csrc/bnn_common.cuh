@@ -190,6 +190,11 @@ bool encode_int32_map(CUtensorMap* map, int32_t* base, int ld, int rows, int col
 // Tensor map of a digit image (digit_gemm.cuh): `chunks` rows of `rows` x 16 bytes, boxes of box_rows x 16 bytes x
 // box_chunks rows, zero fill outside.  Elements are 8 bytes (a box may have at most 256 of them).
 bool encode_digit_map(CUtensorMap* map, const void* base, int rows, int chunks, int box_rows, int box_chunks);
+// Tensor map of the codes of a quantised matrix (f4.cuh): [rows][bytes] with a pitch of `ld` bytes (a multiple of 16, base
+// 16-byte aligned), boxes of 128 bytes x box_rows rows, 128-byte swizzle, zero fill outside.
+bool encode_code_map(CUtensorMap* map, const uint8_t* base, int ld, long long rows, int bytes, int box_rows);
+// Tensor map of its scales: tiles of 512 bytes (base 16-byte aligned), boxes of box_tiles consecutive ones.
+bool encode_scale_map(CUtensorMap* map, const uint8_t* base, long long tiles, int box_tiles);
 // Reads (synchronously) the word that a tensor-core kernel sets when a bounded wait ran out.
 int read_tc_status(int* out);
 // The same as a copy enqueued on `st` (dst: device or pinned host memory), and the reset of the word.

@@ -1,0 +1,385 @@
+// Routing of tokens to experts, and the weighted sum of the experts' results.
+//
+// Router: the k largest logits of a token (ties: the lowest expert), their softmax weights, and a counting sort of the T * k
+// (token, expert) pairs by expert, stable in the token: slot = offsets[expert] + how many earlier tokens chose it.  A warp takes a
+// token, its logits in registers as ordered integers; a pick is two warp reductions.  Within a block's tokens an expert has a
+// bit mask of the tokens that chose it, so that a rank is a popcount and no order of atomics can change a result.  Up to
+// kOneBlock tokens one block does it all; beyond, a first kernel chooses and counts by block, and a second one adds the
+// counts of the blocks before (behind a kernel that sums them, where there are many) and places.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "f4.cuh"
+
+namespace bnn {
+namespace {
+
+constexpr int THREADS = 1024, WARPS = THREADS / 32;
+constexpr int kOneBlock = 128;          // tokens
+constexpr int kMaxChunk = 512;          // tokens of a block: 64 KB of masks for 1024 experts
+constexpr int kManyBlocks = 160;        // from here on the counts are summed by a kernel of their own
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__half* p, float v) { *p = __float2half_rn(v); }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// fp32 <-> unsigned in the same order; 0 stands for "not to be chosen" (-inf, NaN).  -0 is made +0 first: they tie.
+__device__ __forceinline__ uint32_t key_of(float x) {
+    if (!(x > -INFINITY)) return 0u;
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t key) {
+    return key & 0x80000000u ? __uint_as_float(key & 0x7FFFFFFFu) : __uint_as_float(~key);
+}
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+    return x;
+}
+
+struct Args {
+    const void* logits;
+    int T, E, k, mode, chunk, words, blocks;
+    long long ld;
+    int32_t *index, *offsets, *slot, *source;
+    float* weight;
+    int32_t* counts;       // [blocks][E], then [E] sums
+    int summed;            // counts hold the sums of the blocks before
+};
+
+// A warp's token: lane j < k keeps the j-th choice (-1: none) and its weight.
+template <typename T, int V>
+__device__ __forceinline__ int choose(const T* x, const Args& g, int lane, float* weight) {
+    uint32_t key[V];
+    bool bad = false;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int e = v * 32 + lane;
+        const float f = e < g.E ? to_f32(x[e]) : -INFINITY;
+        bad |= f != f;
+        key[v] = key_of(f);
+    }
+    bad = __any_sync(0xFFFFFFFFu, bad);
+    float total = 0.0f, first = 0.0f;
+    uint32_t kept = 0u;
+    int expert = -1;
+    for (int j = 0; j < g.k; ++j) {
+        uint32_t most = key[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) most = max(most, key[v]);
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        if (most == 0u) break;
+        if (j == 0) {
+            first = value_of(most);
+            if (g.mode == BNN_ROUTE_SOFTMAX) {
+                float part = 0.0f;
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (key[v]) part += expf(value_of(key[v]) - first);
+                total = warp_sum(part);
+            }
+        }
+        int e = 0x7FFFFFFF;
+#pragma unroll
+        for (int v = V - 1; v >= 0; --v)
+            if (key[v] == most) e = v * 32 + lane;
+        e = (int)__reduce_min_sync(0xFFFFFFFFu, (unsigned)e);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v * 32 + lane == e) key[v] = 0u;
+        if (lane == j) {
+            kept = most;
+            expert = e;
+        }
+    }
+    const float part = expert >= 0 ? expf(value_of(kept) - first) : 0.0f;
+    if (g.mode == BNN_ROUTE_SOFTMAX_CHOSEN) total = warp_sum(part);
+    *weight = expert < 0 ? 0.0f : bad ? __uint_as_float(0x7FC00000u) : part / total;
+    return expert;
+}
+
+// Bits of the masks -> exclusive sums over the experts in base[], by the first warp; returns the sum of all.
+__device__ __forceinline__ void scan_experts(int* base, int E, int32_t* offsets, int lane) {
+    int before = 0;
+    for (int e0 = 0; e0 < E; e0 += 32) {
+        const int e = e0 + lane, mine = e < E ? base[e] : 0;
+        int sum = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+            if (lane >= d) sum += o;
+        }
+        if (e < E) {
+            base[e] = before + sum - mine;
+            if (offsets) offsets[e] = before + sum - mine;
+        }
+        before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    }
+    if (offsets && lane == 0) offsets[E] = before;
+}
+
+__device__ __forceinline__ void place(const Args& g, const uint32_t* mask, const int* base, int first, int n) {
+    for (int i = threadIdx.x; i < n * g.k; i += THREADS) {
+        const int tl = i / g.k;
+        const size_t at = (size_t)first * g.k + i;
+        const int e = g.index[at];
+        int where = -1;
+        if (e >= 0) {
+            const uint32_t* m = mask + e * g.words;
+            where = base[e] + __popc(m[tl >> 5] & ((1u << (tl & 31)) - 1u));
+            for (int w = 0; w < tl >> 5; ++w) where += __popc(m[w]);
+            g.source[where] = first + tl;
+        }
+        g.slot[at] = where;
+    }
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(THREADS) choose_kernel(const __grid_constant__ Args g) {
+    extern __shared__ uint32_t mask[];           // [E][words], then base[E]
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < g.E * g.words; i += THREADS) mask[i] = 0u;
+    pdl_wait();
+    __syncthreads();
+    const int first = blockIdx.x * g.chunk, n = min(g.chunk, g.T - first);
+    for (int t = warp; t < n; t += WARPS) {
+        float weight;
+        const int e = choose<T, V>(static_cast<const T*>(g.logits) + (first + t) * g.ld, g, lane, &weight);
+        if (lane < g.k) {
+            const size_t at = (size_t)(first + t) * g.k + lane;
+            g.index[at] = e;
+            g.weight[at] = weight;
+            if (e >= 0) atomicOr(mask + e * g.words + (t >> 5), 1u << (t & 31));
+        }
+    }
+    __syncthreads();
+    int* base = reinterpret_cast<int*>(mask + g.E * g.words);
+    for (int e = threadIdx.x; e < g.E; e += THREADS) {
+        int c = 0;
+        for (int w = 0; w < g.words; ++w) c += __popc(mask[e * g.words + w]);
+        if (g.blocks > 1) g.counts[(size_t)blockIdx.x * g.E + e] = c;
+        else base[e] = c;
+    }
+    if (g.blocks > 1) return;
+    __syncthreads();
+    if (warp == 0) scan_experts(base, g.E, g.offsets, lane);
+    __syncthreads();
+    place(g, mask, base, first, n);
+}
+
+// counts[b][e] -> the sum over the blocks before b, and behind them the sums over all; 32 experts a block, its warps share
+// the blocks.
+__global__ void __launch_bounds__(THREADS) sum_kernel(const __grid_constant__ Args g) {
+    __shared__ int part[WARPS][33];
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
+    const int each = ceil_div(g.blocks, WARPS), lo = min(warp * each, g.blocks), hi = min(lo + each, g.blocks);
+    int sum = 0;
+    if (e < g.E)
+        for (int b = lo; b < hi; ++b) sum += g.counts[(size_t)b * g.E + e];
+    part[warp][lane] = sum;
+    __syncthreads();
+    int before = 0;
+    for (int w = 0; w < warp; ++w) before += part[w][lane];
+    if (e < g.E) {
+        for (int b = lo; b < hi; ++b) {
+            const int c = g.counts[(size_t)b * g.E + e];
+            g.counts[(size_t)b * g.E + e] = before;
+            before += c;
+        }
+        if (warp == WARPS - 1) g.counts[(size_t)g.blocks * g.E + e] = before;
+    }
+}
+
+__global__ void __launch_bounds__(THREADS) place_kernel(const __grid_constant__ Args g) {
+    extern __shared__ uint32_t mask[];           // [E][words], then base[E] and total[E]
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int* base = reinterpret_cast<int*>(mask + g.E * g.words);
+    int* total = base + g.E;
+    for (int i = threadIdx.x; i < g.E * (g.words + 2); i += THREADS) mask[i] = 0u;
+    pdl_wait();
+    __syncthreads();
+    const int first = blockIdx.x * g.chunk, n = min(g.chunk, g.T - first), mine = blockIdx.x;
+    for (int i = threadIdx.x; i < n * g.k; i += THREADS) {
+        const int e = g.index[(size_t)first * g.k + i], t = i / g.k;
+        if (e >= 0) atomicOr(mask + e * g.words + (t >> 5), 1u << (t & 31));
+    }
+    if (g.summed) {
+        for (int e = threadIdx.x; e < g.E; e += THREADS) {
+            base[e] = g.counts[(size_t)mine * g.E + e];
+            total[e] = g.counts[(size_t)g.blocks * g.E + e];
+        }
+    } else {
+        // threads of a team have an expert each, teams share the blocks; integer sums, whose order is free
+        const int width = min(THREADS, (g.E + 31) & ~31), teams = THREADS / width, team = threadIdx.x / width;
+        const int e = threadIdx.x - team * width;
+        if (e < g.E && team < teams) {
+            int before = 0, all = 0;
+#pragma unroll 4
+            for (int b = team; b < g.blocks; b += teams) {
+                const int c = __ldcg(g.counts + (size_t)b * g.E + e);
+                all += c;
+                before += b < mine ? c : 0;
+            }
+            if (before) atomicAdd(base + e, before);
+            if (all) atomicAdd(total + e, all);
+        }
+    }
+    __syncthreads();
+    if (warp == 0) scan_experts(total, g.E, mine == 0 ? g.offsets : nullptr, lane);
+    __syncthreads();
+    for (int e = threadIdx.x; e < g.E; e += THREADS) base[e] += total[e];
+    __syncthreads();
+    place(g, mask, base, first, n);
+}
+
+struct Plan {
+    int chunk, blocks;
+};
+Plan plan_of(int T) {
+    if (T <= kOneBlock) return {kOneBlock, 1};
+    int chunk = 32 * ceil_div(T, 148 * 32);          // a block an SM, until its masks get large
+    if (chunk > kMaxChunk) chunk = kMaxChunk;
+    return {chunk, ceil_div(T, chunk)};
+}
+
+template <typename T>
+void (*chooser(int E))(Args) {
+    if (E <= 32) return choose_kernel<T, 1>;
+    if (E <= 64) return choose_kernel<T, 2>;
+    if (E <= 128) return choose_kernel<T, 4>;
+    if (E <= 256) return choose_kernel<T, 8>;
+    if (E <= 512) return choose_kernel<T, 16>;
+    return choose_kernel<T, 32>;
+}
+
+// ---- weighted sum ----
+constexpr int SUM_THREADS = 128;
+
+template <typename TZ, bool VEC>
+__device__ __forceinline__ void load8(const TZ* p, int n, float (&v)[8]) {
+    if constexpr (VEC && sizeof(TZ) == 4) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else if constexpr (VEC) {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            TZ h[2];
+            memcpy(h, &w[i], 4);
+            v[2 * i] = to_f32(h[0]);
+            v[2 * i + 1] = to_f32(h[1]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.0f;
+    }
+}
+
+// Block = one token and 1024 columns (8 a lane); the rows of four choices are in flight at once.  VEC: 16-byte accesses, and
+// the width is a multiple of 8.
+template <typename TZ, typename TY, bool VEC>
+__global__ void __launch_bounds__(SUM_THREADS) combine_kernel(const __grid_constant__ CombineArgs g, int turns) {
+    pdl_trigger();
+    pdl_wait();
+    const int t = blockIdx.x / turns, c = ((blockIdx.x - t * turns) * SUM_THREADS + threadIdx.x) * 8;
+    if (c >= g.N) return;
+    float acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+    const TZ* z = static_cast<const TZ*>(g.Z) + c;
+    for (int j0 = 0; j0 < g.k; j0 += 4) {
+        float v[4][8], w[4];
+        bool there[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const size_t at = (size_t)t * g.k + j0 + j;
+            const int s = j0 + j < g.k ? __ldg(g.slot + at) : -1;
+            there[j] = s >= 0 && s < g.rows;
+            w[j] = there[j] ? __ldg(g.weight + at) : 0.0f;
+            if (there[j]) load8<TZ, VEC>(z + (long long)s * g.ldz, g.N - c, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (there[j])
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], v[j][i], acc[i]);
+    }
+    TY* y = static_cast<TY*>(g.Y) + (long long)t * g.ldy + c;
+    if constexpr (VEC && sizeof(TY) == 4) {
+        reinterpret_cast<float4*>(y)[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        reinterpret_cast<float4*>(y)[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    } else if constexpr (VEC) {
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            TY h[2];
+            put(&h[0], acc[2 * i]);
+            put(&h[1], acc[2 * i + 1]);
+            memcpy(&o[i], h, 4);
+        }
+        *reinterpret_cast<uint4*>(y) = make_uint4(o[0], o[1], o[2], o[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < g.N) put(y + i, acc[i]);
+    }
+}
+
+template <typename TZ>
+void (*combiner(int y_dtype, bool vec))(CombineArgs, int) {
+    if (y_dtype == BNN_DTYPE_F32) return vec ? combine_kernel<TZ, float, true> : combine_kernel<TZ, float, false>;
+    if (y_dtype == BNN_DTYPE_F16) return vec ? combine_kernel<TZ, __half, true> : combine_kernel<TZ, __half, false>;
+    return vec ? combine_kernel<TZ, __nv_bfloat16, true> : combine_kernel<TZ, __nv_bfloat16, false>;
+}
+
+}  // namespace
+
+size_t route_workspace_bytes(int T, int E) {
+    const Plan p = plan_of(T);
+    return p.blocks > 1 ? (size_t)(p.blocks + 1) * E * sizeof(int32_t) : 4;
+}
+
+int launch_route(const RouteArgs& a, cudaStream_t st) {
+    const Plan p = plan_of(a.T);
+    Args g{};
+    g.logits = a.logits; g.T = a.T; g.E = a.E; g.k = a.k; g.mode = a.mode; g.ld = a.ld;
+    g.chunk = p.chunk; g.words = p.chunk / 32; g.blocks = p.blocks;
+    g.index = a.index; g.offsets = a.offsets; g.slot = a.slot; g.source = a.source; g.weight = a.weight;
+    g.counts = static_cast<int32_t*>(a.workspace);
+    g.summed = p.blocks >= kManyBlocks;
+    const size_t smem = (size_t)a.E * (g.words + 2) * sizeof(uint32_t);
+    const int most = f4::kMaxGroups * (kMaxChunk / 32 + 2) * (int)sizeof(uint32_t);
+    void (*choose)(Args) = a.dtype == BNN_DTYPE_F32 ? chooser<float>(a.E) : a.dtype == BNN_DTYPE_F16 ? chooser<__half>(a.E) : chooser<__nv_bfloat16>(a.E);
+    if (!ensure_dynamic_smem(reinterpret_cast<const void*>(choose), most) ||
+        !ensure_dynamic_smem(reinterpret_cast<const void*>(place_kernel), most))
+        return BNN_ERR_CUDA;
+    if (launch_pdl(choose, dim3(p.blocks), dim3(THREADS), smem, st, g) != cudaSuccess) return BNN_ERR_CUDA;
+    if (p.blocks > 1) {
+        if (g.summed && launch_pdl(sum_kernel, dim3(ceil_div(a.E, 32)), dim3(THREADS), 0, st, g) != cudaSuccess) return BNN_ERR_CUDA;
+        if (launch_pdl(place_kernel, dim3(p.blocks), dim3(THREADS), smem, st, g) != cudaSuccess) return BNN_ERR_CUDA;
+    }
+    return launch_status();
+}
+
+int launch_combine(const CombineArgs& a, cudaStream_t st) {
+    const int zs = a.dtype == BNN_DTYPE_F32 ? 4 : 2, ys = a.y_dtype == BNN_DTYPE_F32 ? 4 : 2;
+    const bool vec = a.N % 8 == 0 && aligned16(a.Z) && aligned16(a.Y) && ((long long)a.ldz * zs) % 16 == 0 && ((long long)a.ldy * ys) % 16 == 0;
+    const int turns = ceil_div(a.N, SUM_THREADS * 8);
+    if ((long long)a.T * turns > 0x7FFFFFFF) return BNN_ERR_SHAPE;
+    void (*kern)(CombineArgs, int) = a.dtype == BNN_DTYPE_F32 ? combiner<float>(a.y_dtype, vec)
+                                   : a.dtype == BNN_DTYPE_F16 ? combiner<__half>(a.y_dtype, vec) : combiner<__nv_bfloat16>(a.y_dtype, vec);
+    if (launch_pdl(kern, dim3((unsigned)(a.T * turns)), dim3(SUM_THREADS), 0, st, a, turns) != cudaSuccess) return BNN_ERR_CUDA;
+    return launch_status();
+}
+
+}  // namespace bnn

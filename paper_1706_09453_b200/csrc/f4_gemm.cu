@@ -1,0 +1,406 @@
+// Product of two quantised matrices, dense or by groups of rows (experts), on the block-scaled 4-bit tensor-core path:
+//   Y[m][n] = act(scale[n] * 2^e * sum_k a[m][k] w[n][k] + shift[n]),  a and w: e2m1 codes times their blocks' scales.
+//
+// The units (rows of W) are the MMA's M side and the activations' rows its N side: an N can be any multiple of 16, so a tile's
+// width follows the rows that a group has, down to a single token, while 128 units always fill the M side.  The accumulator then
+// has a unit in each lane, and a warp stores 32 consecutive units of a row.
+//
+// Roles of a CTA: one thread copies the stages (256 positions of K: 128 bytes of each row of codes, and their scale tiles)
+// with TMA, one warp moves the scales to tensor memory (tcgen05.cp) and issues the MMAs, eight warps empty the accumulator.
+// Two accumulators alternate.  Tiles of 256 columns leave 512 - 2 * 256 = 0 columns for the scales, so these accumulators
+// overlap by 32 columns, which the epilogue reads first: the next tile starts as soon as they are read.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "f4.cuh"
+#include "tcgen05.cuh"
+
+namespace bnn {
+namespace {
+
+using namespace tc;
+
+constexpr int BM = 128;                  // units of a CTA's tile
+constexpr int BK_BYTES = 128;            // bytes of codes of a row in a stage
+constexpr int BK = 256;
+constexpr int EPI_WARPS = 8, TMA_WARP = 8, MMA_WARP = 9, THREADS = 320;
+constexpr int TMEM_COLS = 512, SF_COL = 480;
+constexpr int SMEM_LIMIT = 232448;
+
+template <bool MX, bool PAIR, int TN>
+struct Shape {
+    static constexpr int KATOMS = MX ? 2 : 4;                     // scale tiles (four blocks of K) of a stage
+    static constexpr int B_ROWS = PAIR ? TN / 2 : TN;             // rows of activations in this CTA's shared memory
+    static constexpr int BOX = B_ROWS >= 128 ? 64 : 32;           // rows of one copy
+    static constexpr int ROW_TILES = TN > 128 ? 2 : 1;            // scale tiles across the activations' rows
+    static constexpr int A_BYTES = BM * BK_BYTES, B_BYTES = B_ROWS * BK_BYTES;
+    static constexpr int SFA_BYTES = KATOMS * 512, SFB_BYTES = ROW_TILES * KATOMS * 512;
+    static constexpr int STAGE = A_BYTES + B_BYTES + SFA_BYTES + SFB_BYTES;
+    static constexpr int CONTROL = 4096 + (f4::kMaxGroups + 1) * 8;
+    static constexpr int FIT = (SMEM_LIMIT - 1024 - CONTROL) / STAGE;
+    static constexpr int STAGES = FIT > 10 ? 10 : FIT;
+    static constexpr int SMEM = STAGES * STAGE + CONTROL + 1024;
+    static constexpr int ACC_STEP = TN > 224 ? SF_COL - TN : TN;  // second accumulator's first column
+    static constexpr int OVERLAP = ACC_STEP < TN ? TN - ACC_STEP : 0;
+    static_assert(STAGE % 1024 == 0 && STAGES >= 3 && ACC_STEP + TN <= SF_COL && (OVERLAP == 0 || OVERLAP == 32), "");
+};
+
+struct Maps {
+    CUtensorMap w, a, w_scales, a_scales;
+};
+
+struct Args {
+    const int32_t* offsets;
+    int groups, M, N, K, kt;
+    float factor;
+    const float* scale;
+    const float* shift;
+    int act, sign_mode;
+    void* Y;
+    int dtype;
+    long long ldy;
+    uint32_t* out_bits;
+    long long ldob;
+    TcStatus status;
+};
+
+struct Control {
+    uint64_t full[10], empty[10], acc_full, acc_free;
+    WaitState wait;
+    uint32_t tmem_base;
+    int first[f4::kMaxGroups + 1];      // first row of each group, held inside 0 .. M
+    int tiles[f4::kMaxGroups + 1];      // row tiles of all groups before
+};
+static_assert(sizeof(Control) <= 4096 + (f4::kMaxGroups + 1) * 8, "");
+
+struct Tile {
+    int g, row0, n, unit0, a_tile;
+};
+
+// Tile number w: units run fastest, so that CTAs that run at the same time share the activations' rows and a group's
+// weights are read by neighbours in time.
+template <int TN>
+__device__ __forceinline__ Tile tile_at(const Control* ctl, const Args& g, int w, int unit_tiles, int unit_step) {
+    const int j = w / unit_tiles;
+    Tile t;
+    t.unit0 = (w - j * unit_tiles) * unit_step;
+    int lo = 0, hi = g.groups;               // the last group whose tiles start at or before j
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (ctl->tiles[mid] <= j) lo = mid; else hi = mid;
+    }
+    t.g = lo;
+    const int off = (j - ctl->tiles[lo]) * TN, begin = ctl->first[lo];
+    t.row0 = begin + off;
+    t.n = min(TN, ctl->first[lo + 1] - t.row0);
+    t.a_tile = begin / 128 + lo + off / 128;
+    return t;
+}
+
+template <bool PAIR>
+__device__ __forceinline__ int columns_of(int n) { return PAIR ? (n + 31) & ~31 : (n + 15) & ~15; }
+
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__half* p, float v) { *p = __float2half_rn(v); }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ float activate(float v, int act) {
+    if (act == BNN_ACT_HARDTANH) return fminf(fmaxf(v, -1.0f), 1.0f) + (v != v ? v : 0.0f);
+    if (act == BNN_ACT_SIGMOID) return 1.0f / (1.0f + expf(-v));
+    return v;
+}
+
+// One chunk of 32 columns (rows of the result) of a lane's unit.
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* y, long long ldy, const uint32_t (&acc)[32], int n, float factor, float scale, float shift, int act) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        if (i < n) put(y + i * ldy, activate(fmaf(scale, __uint_as_float(acc[i]) * factor, shift), act));
+}
+
+template <bool MX, bool PAIR, int TN>
+__device__ __forceinline__ void body(const Maps& maps, const Args& g) {
+    using S = Shape<MX, PAIR, TN>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    Control* ctl = reinterpret_cast<Control*>(smem + S::STAGES * S::STAGE);
+    volatile int* abort_flag = &ctl->wait.abort;
+    pdl_trigger();
+    const int warp = warp_index(), lane = threadIdx.x & 31;
+    const int rank = PAIR ? (int)cluster_rank() : 0;
+    constexpr int CTAS = PAIR ? 2 : 1;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::STAGES; ++s) {
+            mbar_init(smem_u32(&ctl->full[s]), 1);      // (rank 0:) its copying thread, and the bytes of both CTAs
+            mbar_init(smem_u32(&ctl->empty[s]), 1);     // a commit
+        }
+        mbar_init(smem_u32(&ctl->acc_full), 1);
+        mbar_init(smem_u32(&ctl->acc_free), CTAS * EPI_WARPS);
+        wait_state_init(&ctl->wait, g.status);
+        mbar_init_fence();
+    }
+    __syncwarp();
+    if (warp == MMA_WARP) {
+        if constexpr (PAIR) {
+            tmem_alloc_pair(smem_u32(&ctl->tmem_base), TMEM_COLS);
+        } else {
+            tmem_alloc(smem_u32(&ctl->tmem_base), TMEM_COLS);
+            tmem_relinquish();
+        }
+    }
+    pdl_wait();
+    // Groups: offsets that make no sense are held inside the matrix, and a group never ends before it starts.
+    if (g.offsets) {
+        for (int i = threadIdx.x; i <= g.groups; i += THREADS) ctl->first[i] = min(max(__ldg(g.offsets + i), 0), g.M);
+        __syncthreads();
+        if (warp == 0) {
+            int before = 0;
+            for (int i0 = 0; i0 < g.groups; i0 += 32) {
+                const int i = i0 + lane;
+                const int mine = i < g.groups ? (max(ctl->first[i + 1] - ctl->first[i], 0) + TN - 1) / TN : 0;
+                int sum = mine;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int o = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+                    if (lane >= d) sum += o;
+                }
+                if (i < g.groups) ctl->tiles[i] = before + sum - mine;
+                before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+            }
+            if (lane == 0) ctl->tiles[g.groups] = before;
+        }
+    } else if (threadIdx.x == 0) {
+        ctl->first[0] = 0;
+        ctl->first[1] = g.M;
+        ctl->tiles[0] = 0;
+        ctl->tiles[1] = ceil_div(g.M, TN);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if constexpr (PAIR) cluster_sync();
+    tc_fence_after_sync();
+    const uint32_t tmem = ctl->tmem_base;
+
+    const int unit_tiles = ceil_div(g.N, BM * CTAS), nks = ceil_div(g.K, BK);
+    const long long total = (long long)ctl->tiles[g.groups] * unit_tiles;
+    const int step = gridDim.x / CTAS;
+
+    if (warp == TMA_WARP) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 1;
+            bool ok = true;
+            for (long long w = blockIdx.x / CTAS; w < total && ok; w += step) {
+                const Tile t = tile_at<TN>(ctl, g, (int)w, unit_tiles, BM * CTAS);
+                const int cols = columns_of<PAIR>(t.n);
+                const int mine = PAIR ? cols / 2 : cols, boxes = ceil_div(mine, S::BOX);
+                const int unit = t.unit0 + rank * BM, row = t.row0 + rank * mine;
+                const int w_row = t.g * g.N + unit;
+                const int w_tile = (int)((long long)t.g * g.N / 128) + t.g + unit / 128;
+                const uint32_t bytes = S::A_BYTES + boxes * S::BOX * BK_BYTES + S::SFA_BYTES + S::SFB_BYTES;
+                for (int ks = 0; ks < nks; ++ks) {
+                    ok = mbar_wait(smem_u32(&ctl->empty[s]), ph, abort_flag);
+                    if (!ok) break;
+                    const uint32_t dst = smem_u32(smem) + s * S::STAGE, bar = smem_u32(&ctl->full[s]);
+                    const uint32_t bar0 = PAIR ? peer_addr(bar, 0) : bar;
+                    if (rank == 0) mbar_arrive_expect_tx(bar, CTAS * bytes);
+                    auto load = [&](uint32_t to, const CUtensorMap* map, int x, int y) {
+                        if constexpr (PAIR) tma_load_2d_pair(to, map, x, y, bar0);
+                        else tma_load_2d(to, map, x, y, bar);
+                    };
+                    load(dst, &maps.w, ks * BK_BYTES, w_row);
+                    for (int b = 0; b < boxes; ++b) load(dst + S::A_BYTES + b * S::BOX * BK_BYTES, &maps.a, ks * BK_BYTES, row + b * S::BOX);
+                    const uint32_t sf = dst + S::A_BYTES + S::B_BYTES;
+                    load(sf, &maps.w_scales, 0, w_tile * g.kt + ks * S::KATOMS);
+                    for (int b = 0; b < S::ROW_TILES; ++b)
+                        load(sf + S::SFA_BYTES + b * S::KATOMS * 512, &maps.a_scales, 0, (t.a_tile + b) * g.kt + ks * S::KATOMS);
+                    if (++s == S::STAGES) { s = 0; ph ^= 1u; }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == MMA_WARP) {
+        int s = 0, buf = 0;
+        uint32_t ph = 0, pfree = 1;       // a fresh barrier passes parity 1
+        bool ok = rank == 0;
+        for (long long w = blockIdx.x / CTAS; w < total && ok; w += step) {
+            const Tile t = tile_at<TN>(ctl, g, (int)w, unit_tiles, BM * CTAS);
+            const int cols = columns_of<PAIR>(t.n);
+            const uint32_t id0 = instr_desc_f4(BM * CTAS, cols, MX, 0), id2 = instr_desc_f4(BM * CTAS, cols, MX, MX ? 2 : 0);
+            // the accumulator before this one is read as far as this one overlaps it, and all of the one before that
+            ok = warp_wait(smem_u32(&ctl->acc_free), pfree, abort_flag, lane);
+            if (!ok) break;
+            pfree ^= 1u;
+            tc_fence_after_sync();
+            const uint32_t d = tmem + buf * S::ACC_STEP, sfa = tmem + SF_COL, sfb = sfa + 8;
+            for (int ks = 0; ks < nks; ++ks) {
+                ok = warp_wait(smem_u32(&ctl->full[s]), ph, abort_flag, lane);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t base = smem_u32(smem) + s * S::STAGE, sf = base + S::A_BYTES + S::B_BYTES;
+                const uint64_t da = smem_desc_sw128(base), db = smem_desc_sw128(base + S::A_BYTES);
+                const int left = g.K - ks * BK;
+                if (elect_one()) {
+                    // Halves of 128 positions: their scales, then two MMAs of 64.  The copies and MMAs of one thread run in
+                    // order, so the same columns hold the scales of every half.
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (h * 128 >= left) break;
+#pragma unroll
+                        for (int c = 0; c < S::KATOMS / 2; ++c) {
+                            const int katom = h * (S::KATOMS / 2) + c;
+                            tmem_copy_scales<PAIR>(sfa + 4 * c, sf + katom * 512);
+#pragma unroll
+                            for (int b = 0; b < S::ROW_TILES; ++b)
+                                tmem_copy_scales<PAIR>(sfb + 4 * S::ROW_TILES * c + 4 * b, sf + S::SFA_BYTES + (b * S::KATOMS + katom) * 512);
+                        }
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            if (h * 128 + m * 64 >= left) break;
+                            const int x = (h * 2 + m) * 2;       // 32 bytes, in units of 16
+                            mma_f4<MX, PAIR>(d, da + x, db + x, MX && m ? id2 : id0, MX ? sfa : sfa + 4 * m,
+                                             MX ? sfb : sfb + 4 * S::ROW_TILES * m, (ks | h | m) != 0);
+                        }
+                    }
+                    if constexpr (PAIR) mma_commit_pair(smem_u32(&ctl->empty[s]));
+                    else mma_commit(smem_u32(&ctl->empty[s]));
+                }
+                if (++s == S::STAGES) { s = 0; ph ^= 1u; }
+            }
+            if (ok && elect_one()) {
+                if constexpr (PAIR) mma_commit_pair(smem_u32(&ctl->acc_full));
+                else mma_commit(smem_u32(&ctl->acc_full));
+            }
+            buf ^= 1;
+        }
+        __syncwarp();
+    } else {
+        const int half = warp >> 2, quarter = warp & 3;
+        const uint32_t free0 = PAIR ? peer_addr(smem_u32(&ctl->acc_free), 0) : smem_u32(&ctl->acc_free);
+        uint32_t pfull = 0;
+        int buf = 0;
+        for (long long w = blockIdx.x / CTAS; w < total; w += step) {
+            const Tile t = tile_at<TN>(ctl, g, (int)w, unit_tiles, BM * CTAS);
+            const int unit = t.unit0 + rank * BM + quarter * 32 + lane, chunks = ceil_div(t.n, 32);
+            const bool there = unit < g.N;
+            const size_t p = (size_t)t.g * g.N + unit;
+            const float scale = g.scale && there ? __ldg(g.scale + p) : 1.0f, shift = g.shift && there ? __ldg(g.shift + p) : 0.0f;
+            if (!warp_wait_relaxed(smem_u32(&ctl->acc_full), pfull, abort_flag, lane)) break;
+            pfull ^= 1u;
+            tc_fence_after_sync();
+            const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * S::ACC_STEP);
+            bool freed = false;
+            // the columns that the next tile's accumulator overlaps come first: the highest of the first one, the lowest
+            // of the second
+            const int mine = (chunks - half + 1) >> 1;
+#pragma unroll 1
+            for (int i = 0; i < mine; ++i) {
+                const int c = half + 2 * (buf == 0 ? mine - 1 - i : i), n = min(32, t.n - c * 32);
+                uint32_t acc[32];
+                tmem_ld32(taddr + c * 32, acc);
+                tmem_ld_wait();
+                if (!freed) {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (PAIR) mbar_arrive_cluster(free0);
+                        else mbar_arrive(free0);
+                    }
+                    freed = true;
+                }
+                const long long row = t.row0 + c * 32;
+                if (g.out_bits) {
+                    uint32_t word = 0;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const float v = fmaf(scale, __uint_as_float(acc[j]) * g.factor, shift);
+                        const uint32_t b = __ballot_sync(0xFFFFFFFFu, there && sign_is_pos(v, g.sign_mode));
+                        if (lane == j) word = b;
+                    }
+                    const int u0 = t.unit0 + rank * BM + quarter * 32;
+                    if (lane < n && u0 < g.N) g.out_bits[(row + lane) * g.ldob + (u0 >> 5)] = word;
+                } else if (there) {
+                    const long long at = row * g.ldy + unit;
+                    if (g.dtype == BNN_DTYPE_F32) store_chunk(static_cast<float*>(g.Y) + at, g.ldy, acc, n, g.factor, scale, shift, g.act);
+                    else if (g.dtype == BNN_DTYPE_F16) store_chunk(static_cast<__half*>(g.Y) + at, g.ldy, acc, n, g.factor, scale, shift, g.act);
+                    else store_chunk(static_cast<__nv_bfloat16*>(g.Y) + at, g.ldy, acc, n, g.factor, scale, shift, g.act);
+                }
+            }
+            if (!freed) {
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (PAIR) mbar_arrive_cluster(free0);
+                    else mbar_arrive(free0);
+                }
+            }
+            buf ^= 1;
+        }
+    }
+
+    // every thread arrives here, also after a wait that ran out
+    __syncwarp();
+    tc_fence_before_sync();
+    __syncthreads();
+    if constexpr (PAIR) cluster_sync();
+    if (warp == MMA_WARP) {
+        tc_fence_after_sync();
+        if constexpr (PAIR) tmem_dealloc_pair(tmem, TMEM_COLS);
+        else tmem_dealloc(tmem, TMEM_COLS);
+    }
+    if (threadIdx.x == 0 && ctl->wait.abort) atomicExch(g.status.word, 1);
+}
+
+template <bool MX, int TN>
+__global__ void __launch_bounds__(THREADS, 1) f4_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args g) {
+    body<MX, false, TN>(maps, g);
+}
+
+template <typename S>
+bool encode_maps(Maps* m, const F4GemmArgs& a, int kt) {
+    const int bytes = f4::code_bytes(a.K);
+    const long long units = (long long)a.groups * a.N;
+    return encode_code_map(&m->w, a.w, a.ldw, units, bytes, BM) && encode_code_map(&m->a, a.a, a.lda, a.M, bytes, S::BOX) &&
+           encode_scale_map(&m->w_scales, a.w_scales, (long long)(units / 128 + a.groups) * kt, S::KATOMS) &&
+           encode_scale_map(&m->a_scales, a.a_scales, (long long)f4::row_tiles(a.M, a.groups) * kt, S::KATOMS);
+}
+
+template <bool MX, int TN>
+int launch_single(const F4GemmArgs& a, Args g, int sms, cudaStream_t st) {
+    using S = Shape<MX, false, TN>;
+    Maps maps;
+    auto kern = f4_gemm_kernel<MX, TN>;
+    if (!ensure_dynamic_smem(reinterpret_cast<const void*>(kern), S::SMEM) || !encode_maps<S>(&maps, a, g.kt)) return BNN_ERR_CUDA;
+    // an upper bound on the tiles: the groups' rows are only known on the device
+    const long long row_tiles = a.M / TN + (a.offsets ? (a.M < a.groups ? a.M : a.groups) : 1);
+    const long long tiles = row_tiles * ceil_div(a.N, BM);
+    const int grid = (int)(tiles < sms ? tiles : sms);
+    if (launch_pdl(kern, dim3(grid), dim3(THREADS), S::SMEM, st, maps, g) != cudaSuccess) return BNN_ERR_CUDA;
+    return launch_status();
+}
+
+template <bool MX>
+int launch_format(const F4GemmArgs& a, const Args& g, int sms, cudaStream_t st) {
+    const int rows = a.offsets ? ceil_div(a.M, a.groups) : a.M;      // of a group, on average
+    // (a group's second tile of 32 rows would start inside a tile of scales: that form takes 32 rows in all)
+    if (a.M <= 32) return launch_single<MX, 32>(a, g, sms, st);
+    if (rows <= 128) return launch_single<MX, 128>(a, g, sms, st);
+    return launch_single<MX, 256>(a, g, sms, st);
+}
+
+}  // namespace
+
+int launch_f4_gemm(const F4GemmArgs& a, cudaStream_t st) {
+    const int sms = device_sm_count();
+    Args g{};
+    g.offsets = a.offsets; g.groups = a.groups; g.M = a.M; g.N = a.N; g.K = a.K;
+    g.kt = f4::scale_tiles(a.format, a.K);
+    g.factor = a.factor; g.scale = a.scale; g.shift = a.shift; g.act = a.act; g.sign_mode = a.sign_mode;
+    g.Y = a.Y; g.dtype = a.dtype; g.ldy = a.ldy; g.out_bits = a.out_bits; g.ldob = a.ldob;
+    g.status = tc_status();
+    if (sms < 1 || !g.status.word) return BNN_ERR_CUDA;
+    return a.format == BNN_F4_E8M0_32 ? launch_format<true>(a, g, sms, st) : launch_format<false>(a, g, sms, st);
+}
+
+}  // namespace bnn

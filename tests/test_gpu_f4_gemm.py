@@ -1,0 +1,218 @@
+"""Products of quantised matrices, dense and by groups, against 64 bits: every width of a tile, cut blocks, stages and
+tiles, empty groups, rows in no group, the epilogues, and scales that are NaN."""
+import numpy as np
+import pytest
+
+import f4_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    assert torch.cuda.is_available()
+    from paper_1706_09453_b200 import build, binding
+    build.build()
+    return torch, binding
+
+
+def stored(torch, code, byte, offsets=None, groups=1, pad=0):
+    """Device tensors of a quantised matrix; bytes that belong to no row are garbage."""
+    c = ref.pack(code)
+    wide = np.full((c.shape[0], c.shape[1] + 16 * pad), 0xA5, dtype=np.uint8)
+    wide[:, :c.shape[1]] = c
+    return (torch.as_tensor(wide, device=DEV), torch.as_tensor(ref.store_scales(byte, offsets, groups, 0xFF), device=DEV))
+
+
+def product(a, w):
+    """(sums, sums of magnitudes) in 64 bits"""
+    return a @ w.T, np.abs(a) @ np.abs(w).T
+
+
+def bound(total, mag, K, eps):
+    """K additions in fp32 that may cut instead of round, each off by at most a step of a partial sum (2^-23 of the sum of
+    magnitudes), and the rounding to the result's type, half a step of it."""
+    return K * 2.0 ** -23 * mag * (1 + eps) + eps / 2 * np.abs(total) + 1e-30
+
+
+EPS = {"f32": 2.0 ** -23, "f16": 2.0 ** -10, "bf16": 2.0 ** -7}
+
+
+def dtype_of(torch, name):
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+@pytest.mark.parametrize("fmt", [ref.MX, ref.NV])
+@pytest.mark.parametrize("M,N,K", [
+    (1, 1, 1), (1, 128, 32), (1, 130, 64), (2, 5, 33), (1, 2048, 2048), (7, 300, 440), (16, 127, 96), (17, 129, 128), (31, 64, 160), (32, 256, 256),
+    (33, 140, 288), (64, 100, 513), (100, 257, 1000), (128, 128, 384), (129, 384, 224), (200, 77, 640), (255, 200, 31), (256, 128, 512),
+    (257, 300, 100), (300, 129, 1100), (511, 640, 300), (513, 260, 2048), (1100, 900, 700)])
+def test_product(env, fmt, M, N, K):
+    torch, B = env
+    rng = np.random.default_rng(M * 31 + N * 7 + K)
+    a, w = ref.random_stored(rng, M, K, fmt), ref.random_stored(rng, N, K, fmt)
+    (ad, asc), (wd, wsc) = stored(torch, *a, pad=M % 2), stored(torch, *w, pad=N % 2)
+    total, mag = product(ref.values(*a, fmt, K), ref.values(*w, fmt, K))
+    for name in ("f32", "f16", "bf16"):
+        y = torch.full((M + 1, N + 3), 9.0, dtype=dtype_of(torch, name), device=DEV)
+        B.bnn_f4_gemm(ad, asc, wd, wsc, K, y[:M, :N], fmt, exponent=-3)
+        got = y.double().cpu().numpy()
+        assert (got[M] == 9.0).all() and (got[:, N:] == 9.0).all()
+        err = np.abs(got[:M, :N] - total / 8)
+        assert (err <= bound(total / 8, mag / 8, K, EPS[name])).all(), (err / bound(total / 8, mag / 8, K, EPS[name])).max()
+    assert B.bnn_device_status() == 0
+
+
+@pytest.mark.parametrize("fmt", [ref.MX, ref.NV])
+@pytest.mark.parametrize("M,N,K", [(1, 200, 4096), (40, 128, 1000), (300, 300, 2050), (700, 513, 352)])
+def test_sums_that_fp32_holds_are_exact(env, fmt, M, N, K):
+    """Scales of 1: products are multiples of 1/4 and sums stay below 2^22."""
+    torch, B = env
+    rng = np.random.default_rng(K)
+    a, w = ref.random_stored(rng, M, K, fmt, 0), ref.random_stored(rng, N, K, fmt, 0)
+    (ad, asc), (wd, wsc) = stored(torch, *a), stored(torch, *w)
+    y = torch.empty((M, N), device=DEV)
+    B.bnn_f4_gemm(ad, asc, wd, wsc, K, y, fmt)
+    np.testing.assert_array_equal(y.double().cpu().numpy(), product(ref.values(*a, fmt, K), ref.values(*w, fmt, K))[0])
+
+
+@pytest.mark.parametrize("fmt", [ref.MX, ref.NV])
+def test_every_scale_meets_its_block(env, fmt):
+    """One element of A in each row, of another block; W's scales all differ from their neighbours."""
+    torch, B = env
+    rng = np.random.default_rng(3)
+    K, N, n = 1200, 300, ref.BLOCK[fmt]
+    M = -(-K // n)
+    code, byte = np.zeros((M, 2 * ref.pitch(K)), dtype=np.uint8), ref.random_stored(rng, M, K, fmt, 3)[1]
+    code[np.arange(M), np.minimum(np.arange(M) * n + n // 3, K - 1)] = 7
+    w = ref.random_stored(rng, N, K, fmt, 3)
+    (ad, asc), (wd, wsc) = stored(torch, code, byte), stored(torch, *w)
+    y = torch.empty((M, N), device=DEV)
+    B.bnn_f4_gemm(ad, asc, wd, wsc, K, y, fmt)
+    np.testing.assert_array_equal(y.double().cpu().numpy(), product(ref.values(code, byte, fmt, K), ref.values(*w, fmt, K))[0])
+
+
+@pytest.mark.parametrize("fmt", [ref.MX, ref.NV])
+@pytest.mark.parametrize("M", [5, 150, 400])
+def test_epilogues(env, fmt, M):
+    torch, B = env
+    rng = np.random.default_rng(M)
+    N, K = 203, 500
+    a, w = ref.random_stored(rng, M, K, fmt), ref.random_stored(rng, N, K, fmt)
+    (ad, asc), (wd, wsc) = stored(torch, *a), stored(torch, *w)
+    total, mag = product(ref.values(*a, fmt, K), ref.values(*w, fmt, K))
+    scale, shift = rng.normal(0, 0.02, N).astype(np.float32), rng.normal(0, 1, N).astype(np.float32)
+    sc, sh = torch.as_tensor(scale, device=DEV), torch.as_tensor(shift, device=DEV)
+    for use in ("both", "scale", "shift", "none"):
+        s, h = (scale if use in ("both", "scale") else np.ones(N)), (shift if use in ("both", "shift") else np.zeros(N))
+        pre, off = total * s + h, K * 2.0 ** -23 * mag * np.abs(s)
+        kw = dict(scale=sc if use in ("both", "scale") else None, shift=sh if use in ("both", "shift") else None)
+        off = off + 2.0 ** -23 * np.abs(pre) + 1e-30           # the sums, and the rounding of the fused multiply-add
+        y = torch.empty((M, N), device=DEV)
+        B.bnn_f4_gemm(ad, asc, wd, wsc, K, y, fmt, **kw)
+        assert (np.abs(y.double().cpu().numpy() - pre) <= off).all(), use
+        B.bnn_f4_gemm(ad, asc, wd, wsc, K, y, fmt, act=B.ACT_HARDTANH, **kw)
+        assert (np.abs(y.double().cpu().numpy() - np.clip(pre, -1, 1)) <= off).all(), use
+        B.bnn_f4_gemm(ad, asc, wd, wsc, K, y, fmt, act=B.ACT_SIGMOID, **kw)
+        # expf is within 2 steps of 2^-23, the sum and the quotient half a step each; the slope is at most 1/4
+        with np.errstate(over="ignore"):
+            want = 1 / (1 + np.exp(-pre))
+        assert (np.abs(y.double().cpu().numpy() - want) <= off / 4 + 4 * 2.0 ** -23 * want + 1e-30).all(), use
+        for mode in (B.SIGN_ZERO_POS, B.SIGN_ZERO_NEG):
+            bits = torch.full((M + 1, B.packed_pitch(N) + 4), -1, dtype=torch.int32, device=DEV)
+            B.bnn_f4_gemm(ad, asc, wd, wsc, K, None, fmt, act=B.ACT_SIGN_PACK, sign_mode=mode, out_bits=bits[:M], **kw)
+            words = bits.cpu().numpy().view(np.uint32)
+            nw = (N + 31) // 32
+            assert (words[M] == 0xFFFFFFFF).all() and (words[:, nw:] == 0xFFFFFFFF).all()
+            got = (words[:M, :nw, None] >> np.arange(32, dtype=np.uint32) & 1).reshape(M, -1).astype(bool)
+            assert not got[:, N:].any()
+            sure = np.abs(pre) > off
+            assert (got[:, :N] == (pre > 0))[sure].all() and sure.mean() > 0.9
+    assert B.bnn_device_status() == 0
+
+
+def test_sign_of_zero_sums(env):
+    torch, B = env
+    K, M, N = 64, 3, 40
+    code, byte = np.zeros((M, 2 * ref.pitch(K)), dtype=np.uint8), np.full((M, 4), 127, dtype=np.uint8)
+    byte[:, 2:] = 0
+    w = ref.random_stored(np.random.default_rng(0), N, K, ref.MX)
+    (ad, asc), (wd, wsc) = stored(torch, code, byte), stored(torch, *w)
+    for mode, word in ((B.SIGN_ZERO_POS, (0xFFFFFFFF, 0xFF)), (B.SIGN_ZERO_NEG, (0, 0))):
+        bits = torch.zeros((M, 4), dtype=torch.int32, device=DEV)
+        B.bnn_f4_gemm(ad, asc, wd, wsc, K, None, ref.MX, act=B.ACT_SIGN_PACK, sign_mode=mode, out_bits=bits)
+        assert (bits.cpu().numpy().view(np.uint32)[:, :2] == word).all()
+
+
+@pytest.mark.parametrize("fmt", [ref.MX, ref.NV])
+def test_a_scale_that_is_nan_stays_in_its_row(env, fmt):
+    torch, B = env
+    rng = np.random.default_rng(8)
+    for M, N, K in ((3, 130, 96), (150, 200, 300), (400, 140, 512)):
+        a, w = ref.random_stored(rng, M, K, fmt), ref.random_stored(rng, N, K, fmt)
+        nan = 255 if fmt == ref.MX else 127
+        a[1][M // 2, 1], w[1][N - 1, 0] = nan, nan
+        (ad, asc), (wd, wsc) = stored(torch, *a), stored(torch, *w)
+        y = torch.empty((M, N), device=DEV)
+        B.bnn_f4_gemm(ad, asc, wd, wsc, K, y, fmt)
+        want = np.zeros((M, N), dtype=bool)
+        want[M // 2], want[:, N - 1] = True, True
+        np.testing.assert_array_equal(np.isnan(y.cpu().numpy()), want)
+
+
+GROUPS = {
+    "one_row_each": lambda rng: np.arange(41),
+    "mostly_empty": lambda rng: np.array([0] * 9 + [1, 1, 1, 3, 3, 40, 40]),
+    "ragged": lambda rng: np.concatenate([[0], np.cumsum(rng.integers(0, 300, 12))]),
+    "one_large": lambda rng: np.array([0, 2, 1000, 1000, 1001]),
+    "with_rows_outside": lambda rng: np.array([5, 70, 70, 333, 600]),
+    "none": lambda rng: np.zeros(8, dtype=np.int64),
+    "many": lambda rng: np.concatenate([[0], np.sort(rng.integers(0, 1500, 1023)), [1500]]),
+}
+
+
+@pytest.mark.parametrize("fmt", [ref.MX, ref.NV])
+@pytest.mark.parametrize("kind", sorted(GROUPS))
+def test_groups(env, fmt, kind):
+    torch, B = env
+    rng = np.random.default_rng(len(kind))
+    off = GROUPS[kind](rng)
+    G, M = len(off) - 1, max(int(off[-1]), 1) + 7
+    N, K = (33, 70) if G > 100 else (300, 420)
+    a, w = ref.random_stored(rng, M, K, fmt), ref.random_stored(rng, G * N, K, fmt)
+    (ad, asc), (wd, wsc) = stored(torch, *a, offsets=off, groups=G), stored(torch, *w, offsets=np.arange(G + 1) * N, groups=G)
+    av, wv = ref.values(*a, fmt, K), ref.values(*w, fmt, K).reshape(G, N, K)
+    shift = rng.normal(0, 1, (G, N)).astype(np.float32)
+    offd = torch.as_tensor(off.astype(np.int32), device=DEV)
+    for name, sh in (("f32", None), ("bf16", torch.as_tensor(shift, device=DEV))):
+        y = torch.full((M, N), 9.0, dtype=dtype_of(torch, name), device=DEV)
+        B.bnn_f4_gemm_grouped(ad, asc, offd, wd.view(G, N, -1), wsc, K, y, fmt, shift=sh)
+        got = y.double().cpu().numpy()
+        seen = np.zeros(M, dtype=bool)
+        for g in range(G):
+            lo, hi = int(off[g]), int(off[g + 1])
+            seen[lo:hi] = True
+            if hi > lo:
+                total, mag = product(av[lo:hi], wv[g])
+                total = total + (0 if sh is None else shift[g])
+                err, most = np.abs(got[lo:hi] - total), bound(total, mag + np.abs(total), K + 1, EPS[name])
+                assert (err <= most).all(), (g, (err / most).max())
+        assert (got[~seen] == 9.0).all()
+    assert B.bnn_device_status() == 0
+
+
+def test_offsets_that_make_no_sense_stay_inside(env):
+    torch, B = env
+    rng = np.random.default_rng(1)
+    M, N, K = 100, 130, 64
+    for off in ([90, 20, 0], [-5, 10, 1 << 30], [7, -1, 3, 50], [1 << 30, 1 << 30], [0, 100, 0, 100]):
+        G = len(off) - 1
+        a, w = ref.random_stored(rng, M, K, ref.MX), ref.random_stored(rng, G * N, K, ref.MX)
+        ad, asc = stored(torch, *a, groups=G)
+        wd, wsc = stored(torch, *w, offsets=np.arange(G + 1) * N, groups=G)
+        y = torch.full((M + 1, N), 9.0, device=DEV)
+        B.bnn_f4_gemm_grouped(ad, asc, torch.as_tensor(np.array(off, dtype=np.int32), device=DEV), wd.view(G, N, -1), wsc, K, y[:M], ref.MX)
+        assert (y[M] == 9.0).all()
+    assert B.bnn_device_status() == 0
