@@ -240,7 +240,8 @@ def _ld(t):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    # the stream's handle itself: the Stream object that torch.cuda.current_stream() builds takes 3 us of a call's 10
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _check(rc, where):
@@ -503,16 +504,17 @@ _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 def _dtype(t):
-    if t.dtype not in _DTYPES:
+    d = _DTYPES.get(t.dtype)
+    if d is None:
         raise TypeError("expected float32, float16 or bfloat16, got %s" % t.dtype)
-    return _DTYPES[t.dtype]
+    return d
 
 
 def _here(*tensors):
     """All tensors given lie on the device that the call runs on."""
-    dev = torch.cuda.current_device()
+    dev = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
+        if t is not None and t.get_device() != dev:
             raise ValueError("expected a tensor on the current CUDA device %d, got one on %s" % (dev, t.device))
 
 
@@ -523,10 +525,17 @@ def _need(ok, what):
 
 def _flat(t, dtype, n, what):
     """Address of a contiguous tensor of exactly n elements."""
-    if t.dtype != dtype:
-        raise TypeError("%s: expected dtype %s, got %s" % (what, dtype, t.dtype))
-    _need(t.numel() == n and t.is_contiguous(), "%s: expected %d contiguous elements" % (what, n))
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s: expected %d contiguous elements of %s, got %s of %s" % (what, n, dtype, tuple(t.shape), t.dtype))
     return t.data_ptr()
+
+
+def _codes(t, dim=2):
+    """(address, pitch) of rows of codes"""
+    stride = t.stride()
+    if t.dtype is not torch.uint8 or len(stride) != dim or stride[-1] != 1:
+        raise ValueError("codes: expected a %d-D uint8 tensor with contiguous rows" % dim)
+    return t.data_ptr(), stride[-2]
 
 
 def bnn_f4_pitch(K) -> int:
@@ -542,12 +551,14 @@ def _groups(offsets):
     """(address, number of groups)"""
     if offsets is None:
         return None, 1
-    return _flat(offsets, torch.int32, offsets.numel(), "offsets"), offsets.numel() - 1
+    n = offsets.numel()
+    return _flat(offsets, torch.int32, n, "offsets"), n - 1
 
 
 def _scales(t):
     """(address, bytes)"""
-    return _flat(t, torch.uint8, t.numel(), "scales"), t.numel()
+    n = t.numel()
+    return _flat(t, torch.uint8, n, "scales"), n
 
 
 def bnn_f4_quantize(X, codes, scales, fmt=F4_E8M0_32, source=None, offsets=None, exponent=0):
@@ -558,7 +569,7 @@ def bnn_f4_quantize(X, codes, scales, fmt=F4_E8M0_32, source=None, offsets=None,
     sc, sb = _scales(scales)
     src = None if source is None else _flat(source, torch.int32, rows, "source")
     _check(lib().bnn_f4_quantize(X.data_ptr(), _dtype(X), X.shape[0], X.shape[1], _ld(X), src, off, groups, rows, fmt, exponent,
-                                 _ptr(codes, torch.uint8), _ld(codes), sc, sb, _stream()), "bnn_f4_quantize")
+                                 *_codes(codes), sc, sb, _stream()), "bnn_f4_quantize")
     return codes, scales
 
 
@@ -568,7 +579,7 @@ def bnn_f4_dequantize(codes, scales, Y, fmt=F4_E8M0_32, offsets=None, exponent=0
     _need(codes.shape[0] == Y.shape[0], "codes and Y have different numbers of rows")
     off, groups = _groups(offsets)
     sc, sb = _scales(scales)
-    _check(lib().bnn_f4_dequantize(_ptr(codes, torch.uint8), _ld(codes), sc, sb, off, groups, Y.shape[0], Y.shape[1], fmt, exponent,
+    _check(lib().bnn_f4_dequantize(*_codes(codes), sc, sb, off, groups, Y.shape[0], Y.shape[1], fmt, exponent,
                                    Y.data_ptr(), _dtype(Y), _ld(Y), _stream()), "bnn_f4_dequantize")
     return Y
 
@@ -596,7 +607,7 @@ def bnn_f4_gemm(A, a_scales, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0,
     m, n = A.shape[0], W.shape[0]
     (sa, ba), (sw, bw) = _scales(a_scales), _scales(w_scales)
     y, dt, ldy, epi = _f4_output(m, n, Y, act, sign_mode, scale, shift, out_bits, n)
-    _check(lib().bnn_f4_gemm(_ptr(A, torch.uint8), _ld(A), sa, ba, _ptr(W, torch.uint8), _ld(W), sw, bw, m, n, K, fmt, exponent,
+    _check(lib().bnn_f4_gemm(*_codes(A), sa, ba, *_codes(W), sw, bw, m, n, K, fmt, exponent,
                              y, dt, ldy, epi, _stream()), "bnn_f4_gemm")
     return Y if out_bits is None else out_bits
 
@@ -606,12 +617,13 @@ def bnn_f4_gemm_grouped(A, a_scales, offsets, W, w_scales, K, Y=None, fmt=F4_E8M
     """The same by groups of A's rows; ``W``: codes uint8 [groups][N][pitch], ``scale`` / ``shift``: [groups][N]."""
     _here(A, a_scales, offsets, W, w_scales, Y, scale, shift, out_bits)
     off, groups = _groups(offsets)
-    _need(W.dim() == 3 and W.shape[0] == groups and W.stride(2) == 1 and (groups == 1 or W.stride(0) == W.shape[1] * W.stride(1)),
+    shape, stride = W.shape, W.stride()
+    _need(len(shape) == 3 and shape[0] == groups and (groups == 1 or stride[0] == shape[1] * stride[1]),
           "W: expected [%d, N, pitch], the groups one behind the other" % groups)
     m, n = A.shape[0], W.shape[1]
     (sa, ba), (sw, bw) = _scales(a_scales), _scales(w_scales)
     y, dt, ldy, epi = _f4_output(m, n, Y, act, sign_mode, scale, shift, out_bits, groups * n)
-    _check(lib().bnn_f4_gemm_grouped(_ptr(A, torch.uint8), _ld(A), sa, ba, off, groups, _ptr(W, torch.uint8), W.stride(1), sw, bw,
+    _check(lib().bnn_f4_gemm_grouped(*_codes(A), sa, ba, off, groups, *_codes(W, 3), sw, bw,
                                      m, n, K, fmt, exponent, y, dt, ldy, epi, _stream()), "bnn_f4_gemm_grouped")
     return Y if out_bits is None else out_bits
 

@@ -193,8 +193,8 @@ bool encode_digit_map(CUtensorMap* map, const void* base, int rows, int chunks, 
 // Tensor map of the codes of a quantised matrix (f4.cuh): [rows][bytes] with a pitch of `ld` bytes (a multiple of 16, base
 // 16-byte aligned), boxes of 128 bytes x box_rows rows, 128-byte swizzle, zero fill outside.
 bool encode_code_map(CUtensorMap* map, const uint8_t* base, int ld, long long rows, int bytes, int box_rows);
-// Tensor map of its scales: tiles of 512 bytes (base 16-byte aligned), boxes of box_tiles consecutive ones.
-bool encode_scale_map(CUtensorMap* map, const uint8_t* base, long long tiles, int box_tiles);
+// Tensor map of its scales: [row tile][tile along K][512 bytes] (base 16-byte aligned), boxes of box_rows x box_k tiles.
+bool encode_scale_map(CUtensorMap* map, const uint8_t* base, long long row_tiles, int k_tiles, int box_rows, int box_k);
 // Reads (synchronously) the word that a tensor-core kernel sets when a bounded wait ran out.
 int read_tc_status(int* out);
 // The same as a copy enqueued on `st` (dst: device or pinned host memory), and the reset of the word.

@@ -52,49 +52,79 @@ struct Args {
     int summed;            // counts hold the sums of the blocks before
 };
 
-// A warp's token: lane j < k keeps the j-th choice (-1: none) and its weight.
+// A lane's two largest keys among those not yet taken (a bit each), and which they are; of equal keys the lowest comes first.
+template <int V>
+__device__ __forceinline__ void best_two(const uint32_t (&key)[V], uint32_t taken, uint32_t* best, int* at, uint32_t* second, int* at2) {
+    uint32_t b = 0u, s = 0u;
+    int a = 0, a2 = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const uint32_t x = taken >> v & 1u ? 0u : key[v];
+        const bool first = x > b, next = x > s;
+        s = first ? b : next ? x : s;
+        a2 = first ? a : next ? v : a2;
+        b = first ? x : b;
+        a = first ? v : a;
+    }
+    *best = b; *at = a; *second = s; *at2 = a2;
+}
+
+// A warp's token: lane j < k keeps the j-th choice (-1: none) and its weight.  A pick is the maximum of the lanes' best keys; the
+// lane that had it goes on with its second best, and looks for the one after only when that is picked as well.
 template <typename T, int V>
 __device__ __forceinline__ int choose(const T* x, const Args& g, int lane, float* weight) {
     uint32_t key[V];
+    float f[V];
     bool bad = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int e = v * 32 + lane;
-        const float f = e < g.E ? to_f32(x[e]) : -INFINITY;
-        bad |= f != f;
-        key[v] = key_of(f);
+        f[v] = e < g.E ? to_f32(x[e]) : -INFINITY;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        bad |= f[v] != f[v];
+        key[v] = key_of(f[v]);
     }
     bad = __any_sync(0xFFFFFFFFu, bad);
+    uint32_t best, second, taken = 0u;
+    int at, at2;
+    best_two<V>(key, 0u, &best, &at, &second, &at2);
+    bool fresh = true;                 // `second` is known
     float total = 0.0f, first = 0.0f;
     uint32_t kept = 0u;
     int expert = -1;
     for (int j = 0; j < g.k; ++j) {
-        uint32_t most = key[0];
-#pragma unroll
-        for (int v = 1; v < V; ++v) most = max(most, key[v]);
-        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
         if (most == 0u) break;
         if (j == 0) {
             first = value_of(most);
             if (g.mode == BNN_ROUTE_SOFTMAX) {
+                // (the terms' errors, a few 2^-22 of each, do not add up in one direction)
                 float part = 0.0f;
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (key[v]) part += expf(value_of(key[v]) - first);
+                for (int v = 0; v < V; ++v) part += __expf(f[v] - first);
                 total = warp_sum(part);
             }
         }
-        int e = 0x7FFFFFFF;
-#pragma unroll
-        for (int v = V - 1; v >= 0; --v)
-            if (key[v] == most) e = v * 32 + lane;
-        e = (int)__reduce_min_sync(0xFFFFFFFFu, (unsigned)e);
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v * 32 + lane == e) key[v] = 0u;
+        const unsigned who = __ballot_sync(0xFFFFFFFFu, best == most);
+        int e = at * 32 + lane;
+        if (who & (who - 1u)) e = (int)__reduce_min_sync(0xFFFFFFFFu, best == most ? (unsigned)e : 0xFFFFFFFFu);   // a tie
+        else e = __shfl_sync(0xFFFFFFFFu, e, __ffs(who) - 1);
         if (lane == j) {
             kept = most;
             expert = e;
+        }
+        if (lane == (e & 31)) {
+            taken |= 1u << at;
+            if (fresh) {
+                best = second;
+                at = at2;
+                fresh = false;
+            } else {
+                best_two<V>(key, taken, &best, &at, &second, &at2);
+                fresh = true;
+            }
         }
     }
     const float part = expert >= 0 ? expf(value_of(kept) - first) : 0.0f;
@@ -223,11 +253,19 @@ __global__ void __launch_bounds__(THREADS) place_kernel(const __grid_constant__ 
         const int e = threadIdx.x - team * width;
         if (e < g.E && team < teams) {
             int before = 0, all = 0;
-#pragma unroll 4
-            for (int b = team; b < g.blocks; b += teams) {
-                const int c = __ldcg(g.counts + (size_t)b * g.E + e);
-                all += c;
-                before += b < mine ? c : 0;
+            constexpr int BATCH = 16;      // loads in flight
+            for (int b0 = team; b0 < g.blocks; b0 += BATCH * teams) {
+                int c[BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int b = b0 + i * teams;
+                    c[i] = b < g.blocks ? __ldcg(g.counts + (size_t)b * g.E + e) : 0;
+                }
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    all += c[i];
+                    before += b0 + i * teams < mine ? c[i] : 0;
+                }
             }
             if (before) atomicAdd(base + e, before);
             if (all) atomicAdd(total + e, all);
@@ -246,8 +284,8 @@ struct Plan {
 };
 Plan plan_of(int T) {
     if (T <= kOneBlock) return {kOneBlock, 1};
-    int chunk = 32 * ceil_div(T, 148 * 32);          // a block an SM, until its masks get large
-    if (chunk > kMaxChunk) chunk = kMaxChunk;
+    int chunk = ceil_div(T, 148);          // a block an SM, between a warp's worth of tokens and large masks
+    chunk = chunk < 32 ? 32 : chunk > kMaxChunk ? kMaxChunk : chunk;
     return {chunk, ceil_div(T, chunk)};
 }
 
@@ -264,82 +302,135 @@ void (*chooser(int E))(Args) {
 // ---- weighted sum ----
 constexpr int SUM_THREADS = 128;
 
-template <typename TZ, bool VEC>
-__device__ __forceinline__ void load8(const TZ* p, int n, float (&v)[8]) {
-    if constexpr (VEC && sizeof(TZ) == 4) {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else if constexpr (VEC) {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// Eight elements as they are loaded, and as fp32.
+template <typename TZ> struct Raw { uint4 w; };
+template <> struct Raw<float> { float4 a, b; };
+__device__ __forceinline__ void fetch(Raw<float>& r, const float* p) {
+    r.a = __ldg(reinterpret_cast<const float4*>(p));
+    r.b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+}
+template <typename TZ>
+__device__ __forceinline__ void fetch(Raw<TZ>& r, const TZ* p) { r.w = __ldg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ void add(float (&acc)[8], float w, const Raw<float>& r) {
+    const float v[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            TZ h[2];
-            memcpy(h, &w[i], 4);
-            v[2 * i] = to_f32(h[0]);
-            v[2 * i + 1] = to_f32(h[1]);
-        }
-    } else {
+    for (int i = 0; i < 8; ++i) acc[i] = fmaf(w, v[i], acc[i]);
+}
+template <typename TZ>
+__device__ __forceinline__ void add(float (&acc)[8], float w, const Raw<TZ>& r) {
+    const uint32_t u[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.0f;
+    for (int i = 0; i < 4; ++i) {
+        TZ h[2];
+        memcpy(h, &u[i], 4);
+        acc[2 * i] = fmaf(w, to_f32(h[0]), acc[2 * i]);
+        acc[2 * i + 1] = fmaf(w, to_f32(h[1]), acc[2 * i + 1]);
+    }
+}
+__device__ __forceinline__ void store8(float* y, const float (&acc)[8]) {
+    reinterpret_cast<float4*>(y)[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    reinterpret_cast<float4*>(y)[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+}
+template <typename TY>
+__device__ __forceinline__ void store8(TY* y, const float (&acc)[8]) {
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        TY h[2];
+        put(&h[0], acc[2 * i]);
+        put(&h[1], acc[2 * i + 1]);
+        memcpy(&o[i], h, 4);
+    }
+    *reinterpret_cast<uint4*>(y) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// The rows and weights of four of a token's choices; a row that does not exist is -1.
+__device__ __forceinline__ void choices(const CombineArgs& g, int t, int j0, int (&s)[4], float (&w)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const size_t at = (size_t)t * g.k + j0 + j;
+        s[j] = j0 + j < g.k ? __ldg(g.slot + at) : -1;
+        w[j] = j0 + j < g.k ? __ldg(g.weight + at) : 0.0f;
+        if (s[j] >= g.rows) s[j] = -1;
     }
 }
 
-// Block = one token and 1024 columns (8 a lane); the rows of four choices are in flight at once.  VEC: 16-byte accesses, and
-// the width is a multiple of 8.
-template <typename TZ, typename TY, bool VEC>
+// Block = one token and PIECES * 1024 columns; a lane has PIECES times 8 columns, and the rows of four choices are in flight at
+// once.  16-byte accesses: the width is a multiple of 8.
+template <typename TZ, typename TY, int PIECES>
 __global__ void __launch_bounds__(SUM_THREADS) combine_kernel(const __grid_constant__ CombineArgs g, int turns) {
     pdl_trigger();
     pdl_wait();
-    const int t = blockIdx.x / turns, c = ((blockIdx.x - t * turns) * SUM_THREADS + threadIdx.x) * 8;
+    const int t = blockIdx.x / turns, c = ((blockIdx.x - t * turns) * PIECES * SUM_THREADS + threadIdx.x) * 8;
     if (c >= g.N) return;
+    float acc[PIECES][8];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[p][i] = 0.0f;
+    const TZ* z = static_cast<const TZ*>(g.Z) + c;
+    for (int j0 = 0; j0 < g.k; j0 += 4) {
+        Raw<TZ> raw[4][PIECES];
+        int s[4];
+        float w[4];
+        choices(g, t, j0, s, w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (s[j] >= 0)
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p)
+                    if (PIECES == 1 || c + p * SUM_THREADS * 8 < g.N) fetch(raw[j][p], z + (long long)s[j] * g.ldz + p * SUM_THREADS * 8);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (s[j] >= 0)
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) add(acc[p], w[j], raw[j][p]);
+    }
+    TY* y = static_cast<TY*>(g.Y) + (long long)t * g.ldy + c;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p)
+        if (PIECES == 1 || c + p * SUM_THREADS * 8 < g.N) store8(y + p * SUM_THREADS * 8, acc[p]);
+}
+
+// The same element by element, for rows that start anywhere.
+template <typename TZ, typename TY>
+__global__ void __launch_bounds__(SUM_THREADS) combine_any_kernel(const __grid_constant__ CombineArgs g, int turns) {
+    pdl_trigger();
+    pdl_wait();
+    const int t = blockIdx.x / turns, c0 = (blockIdx.x - t * turns) * SUM_THREADS * 8 + threadIdx.x;
     float acc[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
-    const TZ* z = static_cast<const TZ*>(g.Z) + c;
     for (int j0 = 0; j0 < g.k; j0 += 4) {
-        float v[4][8], w[4];
-        bool there[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const size_t at = (size_t)t * g.k + j0 + j;
-            const int s = j0 + j < g.k ? __ldg(g.slot + at) : -1;
-            there[j] = s >= 0 && s < g.rows;
-            w[j] = there[j] ? __ldg(g.weight + at) : 0.0f;
-            if (there[j]) load8<TZ, VEC>(z + (long long)s * g.ldz, g.N - c, v[j]);
-        }
+        int s[4];
+        float w[4];
+        choices(g, t, j0, s, w);
+        float v[4][8];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (there[j])
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = c0 + i * SUM_THREADS;
+                v[j][i] = s[j] >= 0 && c < g.N ? to_f32(static_cast<const TZ*>(g.Z)[(long long)s[j] * g.ldz + c]) : 0.0f;
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (s[j] >= 0)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], v[j][i], acc[i]);
     }
-    TY* y = static_cast<TY*>(g.Y) + (long long)t * g.ldy + c;
-    if constexpr (VEC && sizeof(TY) == 4) {
-        reinterpret_cast<float4*>(y)[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-        reinterpret_cast<float4*>(y)[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-    } else if constexpr (VEC) {
-        uint32_t o[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            TY h[2];
-            put(&h[0], acc[2 * i]);
-            put(&h[1], acc[2 * i + 1]);
-            memcpy(&o[i], h, 4);
-        }
-        *reinterpret_cast<uint4*>(y) = make_uint4(o[0], o[1], o[2], o[3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < g.N) put(y + i, acc[i]);
-    }
+    for (int i = 0; i < 8; ++i)
+        if (c0 + i * SUM_THREADS < g.N) put(static_cast<TY*>(g.Y) + (long long)t * g.ldy + c0 + i * SUM_THREADS, acc[i]);
 }
 
+template <typename TZ, typename TY>
+void (*combiner(int pieces))(CombineArgs, int) {
+    return pieces == 0 ? combine_any_kernel<TZ, TY> : pieces == 1 ? combine_kernel<TZ, TY, 1> : combine_kernel<TZ, TY, 2>;
+}
 template <typename TZ>
-void (*combiner(int y_dtype, bool vec))(CombineArgs, int) {
-    if (y_dtype == BNN_DTYPE_F32) return vec ? combine_kernel<TZ, float, true> : combine_kernel<TZ, float, false>;
-    if (y_dtype == BNN_DTYPE_F16) return vec ? combine_kernel<TZ, __half, true> : combine_kernel<TZ, __half, false>;
-    return vec ? combine_kernel<TZ, __nv_bfloat16, true> : combine_kernel<TZ, __nv_bfloat16, false>;
+void (*combiner(int y_dtype, int pieces))(CombineArgs, int) {
+    return y_dtype == BNN_DTYPE_F32 ? combiner<TZ, float>(pieces) : y_dtype == BNN_DTYPE_F16 ? combiner<TZ, __half>(pieces) : combiner<TZ, __nv_bfloat16>(pieces);
 }
 
 }  // namespace
@@ -353,7 +444,7 @@ int launch_route(const RouteArgs& a, cudaStream_t st) {
     const Plan p = plan_of(a.T);
     Args g{};
     g.logits = a.logits; g.T = a.T; g.E = a.E; g.k = a.k; g.mode = a.mode; g.ld = a.ld;
-    g.chunk = p.chunk; g.words = p.chunk / 32; g.blocks = p.blocks;
+    g.chunk = p.chunk; g.words = ceil_div(p.chunk, 32); g.blocks = p.blocks;
     g.index = a.index; g.offsets = a.offsets; g.slot = a.slot; g.source = a.source; g.weight = a.weight;
     g.counts = static_cast<int32_t*>(a.workspace);
     g.summed = p.blocks >= kManyBlocks;
@@ -374,10 +465,12 @@ int launch_route(const RouteArgs& a, cudaStream_t st) {
 int launch_combine(const CombineArgs& a, cudaStream_t st) {
     const int zs = a.dtype == BNN_DTYPE_F32 ? 4 : 2, ys = a.y_dtype == BNN_DTYPE_F32 ? 4 : 2;
     const bool vec = a.N % 8 == 0 && aligned16(a.Z) && aligned16(a.Y) && ((long long)a.ldz * zs) % 16 == 0 && ((long long)a.ldy * ys) % 16 == 0;
-    const int turns = ceil_div(a.N, SUM_THREADS * 8);
+    // Two pieces a lane where that leaves every SM a few blocks.
+    const int pieces = !vec ? 0 : a.N > SUM_THREADS * 8 && (long long)a.T * ceil_div(a.N, SUM_THREADS * 16) >= 148 * 8 ? 2 : 1;
+    const int turns = ceil_div(a.N, SUM_THREADS * 8 * (pieces == 2 ? 2 : 1));
     if ((long long)a.T * turns > 0x7FFFFFFF) return BNN_ERR_SHAPE;
-    void (*kern)(CombineArgs, int) = a.dtype == BNN_DTYPE_F32 ? combiner<float>(a.y_dtype, vec)
-                                   : a.dtype == BNN_DTYPE_F16 ? combiner<__half>(a.y_dtype, vec) : combiner<__nv_bfloat16>(a.y_dtype, vec);
+    void (*kern)(CombineArgs, int) = a.dtype == BNN_DTYPE_F32 ? combiner<float>(a.y_dtype, pieces)
+                                   : a.dtype == BNN_DTYPE_F16 ? combiner<__half>(a.y_dtype, pieces) : combiner<__nv_bfloat16>(a.y_dtype, pieces);
     if (launch_pdl(kern, dim3((unsigned)(a.T * turns)), dim3(SUM_THREADS), 0, st, a, turns) != cudaSuccess) return BNN_ERR_CUDA;
     return launch_status();
 }

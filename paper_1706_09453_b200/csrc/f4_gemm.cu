@@ -25,24 +25,26 @@ constexpr int BK_BYTES = 128;            // bytes of codes of a row in a stage
 constexpr int BK = 256;
 constexpr int EPI_WARPS = 8, TMA_WARP = 8, MMA_WARP = 9, THREADS = 320;
 constexpr int TMEM_COLS = 512, SF_COL = 480;
-constexpr int SMEM_LIMIT = 232448;
+constexpr int PANEL = 8;
+constexpr int SMEM_LIMIT = 232448, MAX_STAGES = 10;
+constexpr int OUT_CHUNK = 32 * 64;       // a warp's 32 rows x 32 units of 16 bits on their way out
 
 template <bool MX, bool PAIR, int TN>
 struct Shape {
     static constexpr int KATOMS = MX ? 2 : 4;                     // scale tiles (four blocks of K) of a stage
     static constexpr int B_ROWS = PAIR ? TN / 2 : TN;             // rows of activations in this CTA's shared memory
-    static constexpr int BOX = B_ROWS >= 128 ? 64 : 32;           // rows of one copy
     static constexpr int ROW_TILES = TN > 128 ? 2 : 1;            // scale tiles across the activations' rows
     static constexpr int A_BYTES = BM * BK_BYTES, B_BYTES = B_ROWS * BK_BYTES;
     static constexpr int SFA_BYTES = KATOMS * 512, SFB_BYTES = ROW_TILES * KATOMS * 512;
     static constexpr int STAGE = A_BYTES + B_BYTES + SFA_BYTES + SFB_BYTES;
-    static constexpr int CONTROL = 4096 + (f4::kMaxGroups + 1) * 8;
-    static constexpr int FIT = (SMEM_LIMIT - 1024 - CONTROL) / STAGE;
-    static constexpr int STAGES = FIT > 10 ? 10 : FIT;
-    static constexpr int SMEM = STAGES * STAGE + CONTROL + 1024;
+    static constexpr int CONTROL = 512 + (f4::kMaxGroups + 1) * 8;
+    static constexpr int OUT_BYTES = EPI_WARPS * OUT_CHUNK;
+    static constexpr int FIT = (SMEM_LIMIT - 1024 - CONTROL - OUT_BYTES) / STAGE;
+    static constexpr int STAGES = FIT > MAX_STAGES ? MAX_STAGES : FIT;
+    static constexpr int SMEM = STAGES * STAGE + OUT_BYTES + CONTROL + 1024;
     static constexpr int ACC_STEP = TN > 224 ? SF_COL - TN : TN;  // second accumulator's first column
     static constexpr int OVERLAP = ACC_STEP < TN ? TN - ACC_STEP : 0;
-    static_assert(STAGE % 1024 == 0 && STAGES >= 3 && ACC_STEP + TN <= SF_COL && (OVERLAP == 0 || OVERLAP == 32), "");
+    static_assert(STAGE % 1024 == 0 && STAGES >= 3 && ACC_STEP + TN <= SF_COL && (OVERLAP == 0 || OVERLAP == 32) && SMEM <= SMEM_LIMIT, "");
 };
 
 struct Maps {
@@ -55,35 +57,38 @@ struct Args {
     float factor;
     const float* scale;
     const float* shift;
-    int act, sign_mode;
+    int act, sign_mode, box;
     void* Y;
-    int dtype;
+    int dtype, pieces;
     long long ldy;
     uint32_t* out_bits;
     long long ldob;
     TcStatus status;
 };
 
+template <int A> struct Act { static constexpr int value = A; };
+
 struct Control {
-    uint64_t full[10], empty[10], acc_full, acc_free;
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], acc_full, acc_free;
     WaitState wait;
     uint32_t tmem_base;
     int first[f4::kMaxGroups + 1];      // first row of each group, held inside 0 .. M
     int tiles[f4::kMaxGroups + 1];      // row tiles of all groups before
 };
-static_assert(sizeof(Control) <= 4096 + (f4::kMaxGroups + 1) * 8, "");
+static_assert(sizeof(Control) <= 512 + (f4::kMaxGroups + 1) * 8, "");
 
 struct Tile {
     int g, row0, n, unit0, a_tile;
 };
 
-// Tile number w: units run fastest, so that CTAs that run at the same time share the activations' rows and a group's
-// weights are read by neighbours in time.
+// Tile number w: panels of PANEL unit tiles, in which the units run fastest, so that the tiles that run at the same time
+// are about as many unit tiles as row tiles and share both operands' reads.
 template <int TN>
 __device__ __forceinline__ Tile tile_at(const Control* ctl, const Args& g, int w, int unit_tiles, int unit_step) {
-    const int j = w / unit_tiles;
+    const int rows = ctl->tiles[g.groups], panel = w / (rows * PANEL), in = w - panel * rows * PANEL;
+    const int wide = min(PANEL, unit_tiles - panel * PANEL), j = in / wide;
     Tile t;
-    t.unit0 = (w - j * unit_tiles) * unit_step;
+    t.unit0 = (panel * PANEL + in - j * wide) * unit_step;
     int lo = 0, hi = g.groups;               // the last group whose tiles start at or before j
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -104,18 +109,92 @@ __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__half* p, float v) { *p = __float2half_rn(v); }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-__device__ __forceinline__ float activate(float v, int act) {
-    if (act == BNN_ACT_HARDTANH) return fminf(fmaxf(v, -1.0f), 1.0f) + (v != v ? v : 0.0f);
-    if (act == BNN_ACT_SIGMOID) return 1.0f / (1.0f + expf(-v));
+template <int ACT>
+__device__ __forceinline__ float activate(float v) {
+    if (ACT == BNN_ACT_HARDTANH) return v != v ? v : fminf(fmaxf(v, -1.0f), 1.0f);
+    if (ACT == BNN_ACT_SIGMOID) return 1.0f / (1.0f + expf(-v));
     return v;
 }
+__device__ __forceinline__ uint32_t pack2(float a, float b, __half) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
 
-// One chunk of 32 columns (rows of the result) of a lane's unit.
-template <typename T>
-__device__ __forceinline__ void store_chunk(T* y, long long ldy, const uint32_t (&acc)[32], int n, float factor, float scale, float shift, int act) {
+// Where a warp's chunk of 32 units x 32 rows goes: the first unit's address in the first row, how many units and rows exist.
+struct Chunk {
+    float factor;
+    long long ldy;
+    int units, rows;
+};
+
+// A lane has a unit, a store 32 consecutive ones of a row: fp32, and 16 bits where rows start anywhere.
+template <int ACT, typename T, typename F>
+__device__ __forceinline__ void store_units(T* y, const Chunk& c, uint32_t taddr, int lane, float scale, float shift, F&& read) {
+    uint32_t acc[32];
+    tmem_ld32(taddr, acc);
+    tmem_ld_wait();
+    read();
+    if (lane >= c.units) return;
+    y += lane;
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-        if (i < n) put(y + i * ldy, activate(fmaf(scale, __uint_as_float(acc[i]) * factor, shift), act));
+    for (int i = 0; i < 32; ++i) {
+        if (i < c.rows) put(y, activate<ACT>(fmaf(scale, __uint_as_float(acc[i]) * c.factor, shift)));
+        y += c.ldy;
+    }
+}
+
+// 16 bits, rows of Y on 16-byte boundaries: the accumulator comes in the layout of an MMA's result, goes to shared memory
+// transposed (row by row, 64 bytes each) and from there in pieces of 16 bytes: 4 stores to a chunk instead of 32 (8192 x 1024 x
+// 8192: 46 us instead of 88).
+// out: this warp's chunk of shared memory; piece p of row r lies at r * 64 + 16 * (p ^ (r / 2) % 4), so that neither side meets itself
+// in a bank.  scale, shift: of units lane / 4 + 8 i.  `next`: the chunk to load into acc once this one's values are taken.
+struct Frag {
+    uint32_t lo[16], hi[16];
+    __device__ __forceinline__ void load(uint32_t taddr) {
+        tmem_ld_frag32(taddr, lo);
+        tmem_ld_frag32(taddr + (16u << 16), hi);
+    }
+};
+template <int ACT, typename T>
+__device__ __forceinline__ void store_pieces(T* y, const Chunk& c, Frag& acc, int lane, uint32_t out, const float (&scale)[4],
+                                             const float (&shift)[4], bool more, uint32_t next) {
+    uint32_t v[4][4];
+    auto val = [&](uint32_t a, int i) { return activate<ACT>(fmaf(scale[i], __uint_as_float(a) * c.factor, shift[i])); };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[j][0] = pack2(val(acc.lo[4 * j], 0), val(acc.lo[4 * j + 1], 0), T());
+        v[j][1] = pack2(val(acc.lo[4 * j + 2], 1), val(acc.lo[4 * j + 3], 1), T());
+        v[j][2] = pack2(val(acc.hi[4 * j], 2), val(acc.hi[4 * j + 1], 2), T());
+        v[j][3] = pack2(val(acc.hi[4 * j + 2], 3), val(acc.hi[4 * j + 3], 3), T());
+    }
+    if (more) acc.load(next);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int row = 8 * j + (lane & 7);
+        stmatrix4_trans(out + row * 64 + (((lane >> 3) ^ (row >> 1)) & 3) * 16, v[j][0], v[j][1], v[j][2], v[j][3]);
+    }
+    __syncwarp();
+    const int piece = lane & 3, units = c.units - piece * 8;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int row = 8 * j + (lane >> 2);
+        const uint4 w = lds128u(out + row * 64 + ((piece ^ (row >> 1)) & 3) * 16);
+        if (row >= c.rows) continue;
+        T* p = y + row * c.ldy + piece * 8;
+        if (units >= 8) {
+            *reinterpret_cast<uint4*>(p) = w;
+        } else {
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < units) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
+        }
+    }
+    __syncwarp();
 }
 
 template <bool MX, bool PAIR, int TN>
@@ -123,7 +202,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
     using S = Shape<MX, PAIR, TN>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    Control* ctl = reinterpret_cast<Control*>(smem + S::STAGES * S::STAGE);
+    Control* ctl = reinterpret_cast<Control*>(smem + S::STAGES * S::STAGE + S::OUT_BYTES);
     volatile int* abort_flag = &ctl->wait.abort;
     pdl_trigger();
     const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -194,11 +273,11 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
             for (long long w = blockIdx.x / CTAS; w < total && ok; w += step) {
                 const Tile t = tile_at<TN>(ctl, g, (int)w, unit_tiles, BM * CTAS);
                 const int cols = columns_of<PAIR>(t.n);
-                const int mine = PAIR ? cols / 2 : cols, boxes = ceil_div(mine, S::BOX);
+                const int mine = PAIR ? cols / 2 : cols, boxes = ceil_div(mine, g.box);
                 const int unit = t.unit0 + rank * BM, row = t.row0 + rank * mine;
                 const int w_row = t.g * g.N + unit;
                 const int w_tile = (int)((long long)t.g * g.N / 128) + t.g + unit / 128;
-                const uint32_t bytes = S::A_BYTES + boxes * S::BOX * BK_BYTES + S::SFA_BYTES + S::SFB_BYTES;
+                const uint32_t bytes = S::A_BYTES + boxes * g.box * BK_BYTES + S::SFA_BYTES + S::SFB_BYTES;
                 for (int ks = 0; ks < nks; ++ks) {
                     ok = mbar_wait(smem_u32(&ctl->empty[s]), ph, abort_flag);
                     if (!ok) break;
@@ -209,12 +288,15 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
                         if constexpr (PAIR) tma_load_2d_pair(to, map, x, y, bar0);
                         else tma_load_2d(to, map, x, y, bar);
                     };
+                    auto load_scales = [&](uint32_t to, const CUtensorMap* map, int katom, int tile) {
+                        if constexpr (PAIR) tma_load_3d_pair(to, map, 0, katom, tile, bar0);
+                        else tma_load_3d(to, map, 0, katom, tile, bar);
+                    };
                     load(dst, &maps.w, ks * BK_BYTES, w_row);
-                    for (int b = 0; b < boxes; ++b) load(dst + S::A_BYTES + b * S::BOX * BK_BYTES, &maps.a, ks * BK_BYTES, row + b * S::BOX);
+                    for (int b = 0; b < boxes; ++b) load(dst + S::A_BYTES + b * g.box * BK_BYTES, &maps.a, ks * BK_BYTES, row + b * g.box);
                     const uint32_t sf = dst + S::A_BYTES + S::B_BYTES;
-                    load(sf, &maps.w_scales, 0, w_tile * g.kt + ks * S::KATOMS);
-                    for (int b = 0; b < S::ROW_TILES; ++b)
-                        load(sf + S::SFA_BYTES + b * S::KATOMS * 512, &maps.a_scales, 0, (t.a_tile + b) * g.kt + ks * S::KATOMS);
+                    load_scales(sf, &maps.w_scales, ks * S::KATOMS, w_tile);
+                    load_scales(sf + S::SFA_BYTES, &maps.a_scales, ks * S::KATOMS, t.a_tile);
                     if (++s == S::STAGES) { s = 0; ph ^= 1u; }
                 }
             }
@@ -278,63 +360,94 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
     } else {
         const int half = warp >> 2, quarter = warp & 3;
         const uint32_t free0 = PAIR ? peer_addr(smem_u32(&ctl->acc_free), 0) : smem_u32(&ctl->acc_free);
+        const uint32_t out = smem_u32(smem) + S::STAGES * S::STAGE + warp * OUT_CHUNK;
         uint32_t pfull = 0;
         int buf = 0;
         for (long long w = blockIdx.x / CTAS; w < total; w += step) {
             const Tile t = tile_at<TN>(ctl, g, (int)w, unit_tiles, BM * CTAS);
-            const int unit = t.unit0 + rank * BM + quarter * 32 + lane, chunks = ceil_div(t.n, 32);
-            const bool there = unit < g.N;
-            const size_t p = (size_t)t.g * g.N + unit;
-            const float scale = g.scale && there ? __ldg(g.scale + p) : 1.0f, shift = g.shift && there ? __ldg(g.shift + p) : 0.0f;
+            const int u0 = t.unit0 + rank * BM + quarter * 32, chunks = ceil_div(t.n, 32);
+            // per-unit affine: of the lane's unit, or (16-bit results) of units lane / 4 + 8 i
+            const bool pieces = g.pieces;
+            const size_t p = (size_t)t.g * g.N + u0;
+            float scale[4], shift[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int u = pieces ? (lane >> 2) + 8 * i : lane;
+                scale[i] = g.scale && u0 + u < g.N ? __ldg(g.scale + p + u) : 1.0f;
+                shift[i] = g.shift && u0 + u < g.N ? __ldg(g.shift + p + u) : 0.0f;
+            }
             if (!warp_wait_relaxed(smem_u32(&ctl->acc_full), pfull, abort_flag, lane)) break;
             pfull ^= 1u;
             tc_fence_after_sync();
             const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * S::ACC_STEP);
             bool freed = false;
-            // the columns that the next tile's accumulator overlaps come first: the highest of the first one, the lowest
-            // of the second
-            const int mine = (chunks - half + 1) >> 1;
-#pragma unroll 1
-            for (int i = 0; i < mine; ++i) {
-                const int c = half + 2 * (buf == 0 ? mine - 1 - i : i), n = min(32, t.n - c * 32);
-                uint32_t acc[32];
-                tmem_ld32(taddr + c * 32, acc);
-                tmem_ld_wait();
-                if (!freed) {
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (PAIR) mbar_arrive_cluster(free0);
-                        else mbar_arrive(free0);
-                    }
-                    freed = true;
-                }
-                const long long row = t.row0 + c * 32;
-                if (g.out_bits) {
-                    uint32_t word = 0;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const float v = fmaf(scale, __uint_as_float(acc[j]) * g.factor, shift);
-                        const uint32_t b = __ballot_sync(0xFFFFFFFFu, there && sign_is_pos(v, g.sign_mode));
-                        if (lane == j) word = b;
-                    }
-                    const int u0 = t.unit0 + rank * BM + quarter * 32;
-                    if (lane < n && u0 < g.N) g.out_bits[(row + lane) * g.ldob + (u0 >> 5)] = word;
-                } else if (there) {
-                    const long long at = row * g.ldy + unit;
-                    if (g.dtype == BNN_DTYPE_F32) store_chunk(static_cast<float*>(g.Y) + at, g.ldy, acc, n, g.factor, scale, shift, g.act);
-                    else if (g.dtype == BNN_DTYPE_F16) store_chunk(static_cast<__half*>(g.Y) + at, g.ldy, acc, n, g.factor, scale, shift, g.act);
-                    else store_chunk(static_cast<__nv_bfloat16*>(g.Y) + at, g.ldy, acc, n, g.factor, scale, shift, g.act);
-                }
-            }
-            if (!freed) {
+            auto read = [&] {
+                if (freed) return;
+                freed = true;
                 tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) {
                     if constexpr (PAIR) mbar_arrive_cluster(free0);
                     else mbar_arrive(free0);
                 }
+            };
+            // the columns that the next tile's accumulator overlaps come first: the highest of the first one, the lowest
+            // of the second
+            const int mine = (chunks - half + 1) >> 1;
+            Chunk c{g.factor, g.ldy, g.N - u0, 0};
+            auto chunk_at = [&](int i) { return half + 2 * (buf == 0 ? mine - 1 - i : i); };
+            auto by_pieces = [&](auto* y, auto act) {
+                Frag acc;
+                acc.load(taddr + chunk_at(0) * 32);
+#pragma unroll 1
+                for (int i = 0; i < mine; ++i) {
+                    const int at = chunk_at(i);
+                    c.rows = min(32, t.n - at * 32);
+                    tmem_ld_wait();
+                    read();
+                    store_pieces<decltype(act)::value>(y + (t.row0 + at * 32) * g.ldy + u0, c, acc, lane, out, scale, shift, i + 1 < mine,
+                                                       taddr + chunk_at(i + 1) * 32);
+                }
+            };
+            auto by_units = [&](auto* y, auto act) {
+#pragma unroll 1
+                for (int i = 0; i < mine; ++i) {
+                    const int at = chunk_at(i);
+                    c.rows = min(32, t.n - at * 32);
+                    store_units<decltype(act)::value>(y + (t.row0 + at * 32) * g.ldy + u0, c, taddr + at * 32, lane, scale[0], shift[0], read);
+                }
+            };
+            auto typed = [&](auto act) {
+                if (g.dtype == BNN_DTYPE_F32) by_units(static_cast<float*>(g.Y), act);
+                else if (g.dtype == BNN_DTYPE_F16) pieces ? by_pieces(static_cast<__half*>(g.Y), act) : by_units(static_cast<__half*>(g.Y), act);
+                else pieces ? by_pieces(static_cast<__nv_bfloat16*>(g.Y), act) : by_units(static_cast<__nv_bfloat16*>(g.Y), act);
+            };
+            if (mine > 0) {
+                if (g.out_bits) {
+#pragma unroll 1
+                    for (int i = 0; i < mine; ++i) {
+                        const int at = chunk_at(i);
+                        uint32_t acc[32], word = 0;
+                        tmem_ld32(taddr + at * 32, acc);
+                        tmem_ld_wait();
+                        read();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float v = fmaf(scale[0], __uint_as_float(acc[j]) * g.factor, shift[0]);
+                            const uint32_t b = __ballot_sync(0xFFFFFFFFu, lane < c.units && sign_is_pos(v, g.sign_mode));
+                            if (lane == j) word = b;
+                        }
+                        if (lane < t.n - at * 32 && c.units > 0) g.out_bits[(t.row0 + at * 32 + lane) * g.ldob + (u0 >> 5)] = word;
+                    }
+                } else if (g.act == BNN_ACT_NONE) {
+                    typed(Act<BNN_ACT_NONE>());
+                } else if (g.act == BNN_ACT_HARDTANH) {
+                    typed(Act<BNN_ACT_HARDTANH>());
+                } else {
+                    typed(Act<BNN_ACT_SIGMOID>());
+                }
             }
+            read();
             buf ^= 1;
         }
     }
@@ -357,36 +470,56 @@ __global__ void __launch_bounds__(THREADS, 1) f4_gemm_kernel(const __grid_consta
     body<MX, false, TN>(maps, g);
 }
 
-template <typename S>
-bool encode_maps(Maps* m, const F4GemmArgs& a, int kt) {
-    const int bytes = f4::code_bytes(a.K);
-    const long long units = (long long)a.groups * a.N;
-    return encode_code_map(&m->w, a.w, a.ldw, units, bytes, BM) && encode_code_map(&m->a, a.a, a.lda, a.M, bytes, S::BOX) &&
-           encode_scale_map(&m->w_scales, a.w_scales, (long long)(units / 128 + a.groups) * kt, S::KATOMS) &&
-           encode_scale_map(&m->a_scales, a.a_scales, (long long)f4::row_tiles(a.M, a.groups) * kt, S::KATOMS);
+// The same on pairs of CTAs: 256 units x up to 256 rows, half of the rows in the shared memory of each.
+template <bool MX>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+f4_gemm_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args g) {
+    body<MX, true, 256>(maps, g);
 }
 
-template <bool MX, int TN>
-int launch_single(const F4GemmArgs& a, Args g, int sms, cudaStream_t st) {
-    using S = Shape<MX, false, TN>;
+template <typename S>
+bool encode_maps(Maps* m, const F4GemmArgs& a, int kt, int box) {
+    const int bytes = f4::code_bytes(a.K);
+    const long long units = (long long)a.groups * a.N;
+    return encode_code_map(&m->w, a.w, a.ldw, units, bytes, BM) && encode_code_map(&m->a, a.a, a.lda, a.M, bytes, box) &&
+           encode_scale_map(&m->w_scales, a.w_scales, units / 128 + a.groups, kt, 1, S::KATOMS) &&
+           encode_scale_map(&m->a_scales, a.a_scales, f4::row_tiles(a.M, a.groups), kt, S::ROW_TILES, S::KATOMS);
+}
+
+template <bool MX, bool PAIR, int TN>
+int launch_form(const F4GemmArgs& a, Args g, int box, int sms, cudaStream_t st) {
+    using S = Shape<MX, PAIR, TN>;
+    constexpr int CTAS = PAIR ? 2 : 1;
     Maps maps;
-    auto kern = f4_gemm_kernel<MX, TN>;
-    if (!ensure_dynamic_smem(reinterpret_cast<const void*>(kern), S::SMEM) || !encode_maps<S>(&maps, a, g.kt)) return BNN_ERR_CUDA;
+    g.box = box;
+    void (*kern)(Maps, Args);
+    if constexpr (PAIR) kern = f4_gemm_pair_kernel<MX>;
+    else kern = f4_gemm_kernel<MX, TN>;
+    if (!ensure_dynamic_smem(reinterpret_cast<const void*>(kern), S::SMEM) || !encode_maps<S>(&maps, a, g.kt, box)) return BNN_ERR_CUDA;
     // an upper bound on the tiles: the groups' rows are only known on the device
     const long long row_tiles = a.M / TN + (a.offsets ? (a.M < a.groups ? a.M : a.groups) : 1);
-    const long long tiles = row_tiles * ceil_div(a.N, BM);
-    const int grid = (int)(tiles < sms ? tiles : sms);
+    const long long tiles = row_tiles * ceil_div(a.N, BM * CTAS);
+    const int grid = CTAS * (int)(tiles < sms / CTAS ? tiles : sms / CTAS);
     if (launch_pdl(kern, dim3(grid), dim3(THREADS), S::SMEM, st, maps, g) != cudaSuccess) return BNN_ERR_CUDA;
     return launch_status();
 }
 
+// Which form.  Up to 32 rows: tiles of 32 (a group's second tile of 32 would start inside a tile of scales, so that these are 32
+// rows in all).  Else single CTAs (128 x 128) or pairs (256 x 256), by the turns that the SMs take and what a turn
+// costs: measured, a pair's is 1.1 (many turns) to 1.25 (one turn) of a single CTA's.  2048 rows, K = N = 2048: pairs 8.7 us, single 10.9;
+// 1024 rows: 9.0 and 7.0; 8192 x 4096 x 8192: 108 and 199.  Groups of less than 128 rows on average are bound by their weights'
+// bytes, and narrow tiles have more of them on their way: 2048 rows by 32 groups 21.2 and 19.3, 4096 rows 27.1 and 27.4.
 template <bool MX>
 int launch_format(const F4GemmArgs& a, const Args& g, int sms, cudaStream_t st) {
+    if (a.M <= 32) return launch_form<MX, false, 32>(a, g, 32, sms, st);
     const int rows = a.offsets ? ceil_div(a.M, a.groups) : a.M;      // of a group, on average
-    // (a group's second tile of 32 rows would start inside a tile of scales: that form takes 32 rows in all)
-    if (a.M <= 32) return launch_single<MX, 32>(a, g, sms, st);
-    if (rows <= 128) return launch_single<MX, 128>(a, g, sms, st);
-    return launch_single<MX, 256>(a, g, sms, st);
+    auto turns = [&](int tile, int ctas) {
+        // (half a tile for the rest of each group)
+        const long long row_tiles = a.offsets ? a.M / tile + (a.groups + 1) / 2 : ceil_div(a.M, tile);
+        return (row_tiles * ceil_div(a.N, BM * ctas) + sms / ctas - 1) / (sms / ctas);
+    };
+    if (rows >= 128 && sms >= 2 && 5 * turns(256, 2) < 4 * turns(128, 1)) return launch_form<MX, true, 256>(a, g, 128, sms, st);
+    return launch_form<MX, false, 128>(a, g, rows <= 32 ? 32 : rows <= 64 ? 64 : 128, sms, st);
 }
 
 }  // namespace
@@ -397,7 +530,8 @@ int launch_f4_gemm(const F4GemmArgs& a, cudaStream_t st) {
     g.offsets = a.offsets; g.groups = a.groups; g.M = a.M; g.N = a.N; g.K = a.K;
     g.kt = f4::scale_tiles(a.format, a.K);
     g.factor = a.factor; g.scale = a.scale; g.shift = a.shift; g.act = a.act; g.sign_mode = a.sign_mode;
-    g.Y = a.Y; g.dtype = a.dtype; g.ldy = a.ldy; g.out_bits = a.out_bits; g.ldob = a.ldob;
+    g.Y = a.Y; g.dtype = a.dtype; g.ldy = a.ldy;
+    g.pieces = a.Y && a.dtype != BNN_DTYPE_F32 && aligned16(a.Y) && a.ldy % 8 == 0; g.out_bits = a.out_bits; g.ldob = a.ldob;
     g.status = tc_status();
     if (sms < 1 || !g.status.word) return BNN_ERR_CUDA;
     return a.format == BNN_F4_E8M0_32 ? launch_format<true>(a, g, sms, st) : launch_format<false>(a, g, sms, st);

@@ -93,6 +93,57 @@ __device__ __forceinline__ bool locate(const int32_t* offsets, int groups, int r
     return true;
 }
 
+// Largest magnitude of eight elements as the bits of an fp32 number (NaNs are above all others).
+__device__ __forceinline__ uint32_t magnitude(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return m;
+}
+// The same from eight 16-bit elements as they were loaded, two at a time.
+__device__ __forceinline__ uint32_t magnitude2(const uint4& w) {
+    const uint32_t keep = 0x7FFF7FFFu;
+    const uint32_t m = __vmaxu2(__vmaxu2(w.x & keep, w.y & keep), __vmaxu2(w.z & keep, w.w & keep));
+    return max(m & 0xFFFFu, m >> 16);
+}
+__device__ __forceinline__ uint32_t widen_magnitude(uint32_t m, __nv_bfloat16) { return m << 16; }
+__device__ __forceinline__ uint32_t widen_magnitude(uint32_t m, __half) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m))); }
+
+// One block's share of a lane: eight elements and the block's largest magnitude -> codes, and the scale's byte.
+template <bool MX>
+__device__ __forceinline__ uint32_t to_block(float (&v)[8], uint32_t most, uint32_t* scale) {
+    const bool finite = most < 0x7F800000u;
+    uint32_t byte, codes;
+    if (MX) {
+        byte = max(most >> 23, 2u) - 2u;
+        const float inverse = __uint_as_float((254u - byte) << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= inverse;
+        codes = to_codes(v);
+    } else {
+        byte = to_e4m3(__fdiv_rn(__uint_as_float(most), 6.0f));
+        const float s = from_e4m3(byte), inverse = __frcp_rn(s);
+        // The quotient to the nearest from the rounded reciprocal (Markstein, IBM J. Res. Dev. 34, 1990): the remainder
+        // is exact in a fused multiply-add, and one correction rounds as a division does.  (It makes +0 of -0.)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float q = v[i] * inverse;
+            v[i] = copysignf(byte ? __fmaf_rn(__fmaf_rn(-q, s, v[i]), inverse, q) : 0.0f, v[i]);
+        }
+        codes = to_codes(v);
+    }
+    *scale = finite ? byte : MX ? 0xFFu : 0x7Fu;
+    return finite ? codes : 0u;
+}
+
+template <bool MX>
+__device__ __forceinline__ uint32_t block_max(uint32_t m) {
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+    if (MX) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+    return m;
+}
+
+// A warp: UNROLL segments of 256 elements of a row.
 template <typename T, bool MX, bool VEC, int UNROLL>
 __global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const __grid_constant__ F4QuantArgs g, int turns, long long items) {
     pdl_trigger();
@@ -100,57 +151,81 @@ __global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const __grid_const
     const int lane = threadIdx.x & 31;
     const long long item = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
     if (item >= items) return;
-    const int row = (int)(item / turns), first = (int)(item % turns) * UNROLL * 256;
+    const int row = (int)(item / turns), first = (int)(item - (long long)row * turns) * UNROLL * 256;
     const int src = g.source ? __ldg(g.source + row) : row;
-    const T* x = static_cast<const T*>(g.X) + (long long)src * g.ldx;
+    const T* x = static_cast<const T*>(g.X) + (long long)src * g.ldx + first + lane * 8;
     const bool there = !g.source || (src >= 0 && src < g.src_rows);
-    float v[UNROLL][8];
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int k = first + u * 256 + lane * 8;
-        load8<VEC>(x + k, there ? g.K - k : 0, v[u]);
-    }
+    constexpr int LANES = MX ? 4 : 2;                     // lanes of a block
+    const int k0 = first + lane * 8, kt = f4::scale_tiles(g.format, g.K);
     int tile, local;
-    if (!locate(g.offsets, g.groups, row, lane, &tile, &local)) return;
-    const int kt = f4::scale_tiles(g.format, g.K), bytes = f4::code_bytes(g.K);
-    constexpr int LANES = MX ? 4 : 2;      // lanes of a block
+    // a lane's blocks are 256 / (8 LANES) apart, as many as fill 256 / (32 LANES) tiles
+    constexpr int TILES = 256 / (32 * LANES);
+    const int block = k0 / (8 * LANES);
+    if (VEC && there && first + UNROLL * 256 <= g.K) {
+        // all of it exists: no test on the way
+        if constexpr (sizeof(T) == 2) {
+            uint4 raw[UNROLL];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int k = first + u * 256 + lane * 8;
-        uint32_t most = 0;
+            for (int u = 0; u < UNROLL; ++u) raw[u] = __ldg(reinterpret_cast<const uint4*>(x + u * 256));
+            if (!locate(g.offsets, g.groups, row, lane, &tile, &local)) return;
+            uint8_t* codes = g.codes + (size_t)row * g.ldc + (k0 >> 1);
+            uint8_t* scales = g.scales + scale_place(tile, kt, block >> 2, local) + (block & 3);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[u][i] *= g.factor;
-            most = max(most, __float_as_uint(v[u][i]) & 0x7FFFFFFFu);
-        }
-        most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-        if (MX) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-        const bool finite = most < 0x7F800000u;
-        uint32_t byte, codes;
-        if (MX) {
-            byte = most >> 23 > 2u ? (most >> 23) - 2u : 0u;
-            const float inverse = __uint_as_float((254u - byte) << 23);
+            for (int u = 0; u < UNROLL; ++u) {
+                float v[8];
+                const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] *= inverse;
-            codes = to_codes(v[u]);
-            if (!finite) byte = 0xFFu;
-        } else {
-            byte = to_e4m3(__fdiv_rn(__uint_as_float(most), 6.0f));
-            const float s = from_e4m3(byte), inverse = __frcp_rn(s);
-            // The quotient to the nearest from the rounded reciprocal (Markstein, IBM J. Res. Dev. 34, 1990): the remainder
-            // is exact in a fused multiply-add, and one correction rounds as a division does.  (It makes +0 of -0.)
+                for (int i = 0; i < 4; ++i) {
+                    T h[2];
+                    memcpy(h, &w[i], 4);
+                    v[2 * i] = to_f32(h[0]);
+                    v[2 * i + 1] = to_f32(h[1]);
+                }
+                uint32_t most;
+                if (g.factor == 1.0f) {
+                    most = widen_magnitude(block_max<MX>(magnitude2(raw[u])), T());
+                } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float q = v[u][i] * inverse;
-                v[u][i] = copysignf(byte ? __fmaf_rn(__fmaf_rn(-q, s, v[u][i]), inverse, q) : 0.0f, v[u][i]);
+                    for (int i = 0; i < 8; ++i) v[i] *= g.factor;
+                    most = block_max<MX>(magnitude(v));
+                }
+                uint32_t byte;
+                *reinterpret_cast<uint32_t*>(codes + u * 128) = to_block<MX>(v, most, &byte);
+                if (lane % LANES == 0) scales[u * TILES * 512] = (uint8_t)byte;
             }
-            codes = to_codes(v[u]);
-            if (!finite) byte = 0x7Fu;
+        } else {
+            float v[UNROLL][8];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) load8<true>(x + u * 256, 8, v[u]);
+            if (!locate(g.offsets, g.groups, row, lane, &tile, &local)) return;
+            uint8_t* codes = g.codes + (size_t)row * g.ldc + (k0 >> 1);
+            uint8_t* scales = g.scales + scale_place(tile, kt, block >> 2, local) + (block & 3);
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[u][i] *= g.factor;
+                uint32_t byte;
+                const uint32_t most = block_max<MX>(magnitude(v[u]));
+                *reinterpret_cast<uint32_t*>(codes + u * 128) = to_block<MX>(v[u], most, &byte);
+                if (lane % LANES == 0) scales[u * TILES * 512] = (uint8_t)byte;
+            }
         }
-        if (!finite) codes = 0u;
+        return;
+    }
+    if (!locate(g.offsets, g.groups, row, lane, &tile, &local)) return;
+    const int bytes = f4::code_bytes(g.K);
+#pragma unroll 1
+    for (int u = 0; u < UNROLL; ++u) {
+        const int k = k0 + u * 256;
+        float v[8];
+        load8<VEC>(x + u * 256, there ? g.K - k : 0, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= g.factor;
+        uint32_t byte;
+        const uint32_t codes = to_block<MX>(v, block_max<MX>(magnitude(v)), &byte);
         if (k >> 1 < bytes) *reinterpret_cast<uint32_t*>(g.codes + (size_t)row * g.ldc + (k >> 1)) = codes;
-        const int block = k / (8 * LANES), katom = block >> 2;
-        if (lane % LANES == 0 && katom < kt) g.scales[scale_place(tile, kt, katom, local) + (block & 3)] = k < g.K ? (uint8_t)byte : (uint8_t)0;
+        const int b = block + u * TILES * 4;
+        if (lane % LANES == 0 && b >> 2 < kt) g.scales[scale_place(tile, kt, b >> 2, local) + (b & 3)] = k < g.K ? (uint8_t)byte : (uint8_t)0;
     }
 }
 
@@ -214,21 +289,30 @@ __global__ void __launch_bounds__(WARPS * 32) dequantize_kernel(const __grid_con
     }
     int tile, local;
     if (!locate(g.offsets, g.groups, row, lane, &tile, &local)) return;
-    T* y = static_cast<T*>(g.Y) + (long long)row * g.ldy;
+    const int k0 = first + lane * 8, block = k0 / (MX ? 32 : 16);
+    constexpr int TILES = MX ? 2 : 4;          // of scales in a segment
+    T* y = static_cast<T*>(g.Y) + (long long)row * g.ldy + k0;
+    const uint8_t* scales = g.scales + scale_place(tile, kt, block >> 2, local) + (block & 3);
+    uint32_t byte[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) byte[u] = k0 + u * 256 < g.K ? __ldg(scales + u * TILES * 512) : 0u;
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-        const int k = first + u * 256 + lane * 8, block = k / (MX ? 32 : 16);
-        if (k >= g.K) continue;
-        const uint32_t byte = __ldg(g.scales + scale_place(tile, kt, block >> 2, local) + (block & 3));
-        const float s = MX ? from_e8m0(byte) : from_e4m3(byte & 0x7Fu);
+        const int n = g.K - k0 - u * 256;
+        if (n <= 0) continue;
+        const float s = MX ? from_e8m0(byte[u]) : from_e4m3(byte[u] & 0x7Fu);
         float v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 p = from_codes(codes[u] >> (8 * i));
-            v[2 * i] = p.x * s * g.factor;
-            v[2 * i + 1] = p.y * s * g.factor;
+            v[2 * i] = p.x * s;
+            v[2 * i + 1] = p.y * s;
         }
-        store8<VEC>(y + k, g.K - k, v);
+        if (g.factor != 1.0f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= g.factor;
+        }
+        store8<VEC>(y + u * 256, n, v);
     }
 }
 

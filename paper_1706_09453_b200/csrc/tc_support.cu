@@ -79,14 +79,14 @@ bool encode_code_map(CUtensorMap* map, const uint8_t* base, int ld, long long ro
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool encode_scale_map(CUtensorMap* map, const uint8_t* base, long long tiles, int box_tiles) {
+bool encode_scale_map(CUtensorMap* map, const uint8_t* base, long long row_tiles, int k_tiles, int box_rows, int box_k) {
     const EncodeFn encode = tensor_map_encoder();
     if (!encode) return false;
-    const cuuint64_t dims[2] = {64u, (cuuint64_t)tiles};
-    const cuuint64_t strides[1] = {512u};
-    const cuuint32_t box[2] = {64u, (cuuint32_t)box_tiles};
-    const cuuint32_t estr[2] = {1u, 1u};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_INT64, 2, const_cast<uint8_t*>(base), dims, strides, box, estr,
+    const cuuint64_t dims[3] = {64u, (cuuint64_t)k_tiles, (cuuint64_t)row_tiles};
+    const cuuint64_t strides[2] = {512u, (cuuint64_t)k_tiles * 512};
+    const cuuint32_t box[3] = {64u, (cuuint32_t)box_k, (cuuint32_t)box_rows};
+    const cuuint32_t estr[3] = {1u, 1u, 1u};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_INT64, 3, const_cast<uint8_t*>(base), dims, strides, box, estr,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

@@ -126,6 +126,20 @@ def test_combine(env, zt, yt, T, k, N):
         assert (got[:, N:] == 9.0).all()
 
 
+def test_combine_rows_further_apart_than_32_bits_hold(env):
+    torch, B = env
+    far, N = 1 << 30, 264
+    z = torch.randn((3, N), device=DEV).to(torch.bfloat16)
+    apart = torch.empty((2 * far + N,), dtype=torch.bfloat16, device=DEV).as_strided((3, N), (far, 1))
+    apart.copy_(z)
+    slot = torch.tensor([[2, 0], [1, 2], [0, -1]], dtype=torch.int32, device=DEV)
+    weight = torch.rand((3, 2), device=DEV)
+    want = B.bnn_combine_experts(z, slot, weight, torch.empty((3, N), dtype=torch.bfloat16, device=DEV))
+    assert torch.equal(B.bnn_combine_experts(apart, slot, weight, torch.empty_like(want)), want)
+    out = torch.empty((2 * far + N,), dtype=torch.bfloat16, device=DEV).as_strided((3, N), (far, 1))
+    assert torch.equal(B.bnn_combine_experts(z, slot, weight, out), want)
+
+
 def experts_layer(torch, B, s):
     """A layer of experts as a program runs it: route, gather and quantise, two products by expert, bring the results back."""
     B.bnn_route_experts(s["logits"], s["index"], s["weight"], s["offsets"], s["slot"], s["source"], s["workspace"], B.ROUTE_SOFTMAX_CHOSEN)

@@ -48,7 +48,9 @@ def dtype_of(torch, name):
 @pytest.mark.parametrize("M,N,K", [
     (1, 1, 1), (1, 128, 32), (1, 130, 64), (2, 5, 33), (1, 2048, 2048), (7, 300, 440), (16, 127, 96), (17, 129, 128), (31, 64, 160), (32, 256, 256),
     (33, 140, 288), (64, 100, 513), (100, 257, 1000), (128, 128, 384), (129, 384, 224), (200, 77, 640), (255, 200, 31), (256, 128, 512),
-    (257, 300, 100), (300, 129, 1100), (511, 640, 300), (513, 260, 2048), (1100, 900, 700)])
+    (257, 300, 100), (300, 129, 1100), (511, 640, 300), (513, 260, 2048), (1100, 900, 700),
+    # enough tiles for pairs of CTAs
+    (1100, 2304, 300), (2050, 1300, 513), (1537, 2561, 64), (2300, 1290, 1100), (1290, 2056, 32)])
 def test_product(env, fmt, M, N, K):
     torch, B = env
     rng = np.random.default_rng(M * 31 + N * 7 + K)
@@ -169,6 +171,8 @@ GROUPS = {
     "one_large": lambda rng: np.array([0, 2, 1000, 1000, 1001]),
     "with_rows_outside": lambda rng: np.array([5, 70, 70, 333, 600]),
     "none": lambda rng: np.zeros(8, dtype=np.int64),
+    "pairs": lambda rng: np.array([3, 300, 1301, 1301, 1302, 2799]),
+    "many_pairs": lambda rng: np.concatenate([[0], np.cumsum(rng.integers(1, 700, 13))]),
     "many": lambda rng: np.concatenate([[0], np.sort(rng.integers(0, 1500, 1023)), [1500]]),
 }
 
@@ -180,7 +184,7 @@ def test_groups(env, fmt, kind):
     rng = np.random.default_rng(len(kind))
     off = GROUPS[kind](rng)
     G, M = len(off) - 1, max(int(off[-1]), 1) + 7
-    N, K = (33, 70) if G > 100 else (300, 420)
+    N, K = (33, 70) if G > 100 else (1300, 200) if "pairs" in kind else (300, 420)
     a, w = ref.random_stored(rng, M, K, fmt), ref.random_stored(rng, G * N, K, fmt)
     (ad, asc), (wd, wsc) = stored(torch, *a, offsets=off, groups=G), stored(torch, *w, offsets=np.arange(G + 1) * N, groups=G)
     av, wv = ref.values(*a, fmt, K), ref.values(*w, fmt, K).reshape(G, N, K)
@@ -216,3 +220,23 @@ def test_offsets_that_make_no_sense_stay_inside(env):
         B.bnn_f4_gemm_grouped(ad, asc, torch.as_tensor(np.array(off, dtype=np.int32), device=DEV), wd.view(G, N, -1), wsc, K, y[:M], ref.MX)
         assert (y[M] == 9.0).all()
     assert B.bnn_device_status() == 0
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_rows_further_apart_than_32_bits_hold(env, name):
+    torch, B = env
+    rng = np.random.default_rng(4)
+    M, N, K, far = 3, 200, 96, 1 << 30
+    a, w = ref.random_stored(rng, M, K, ref.MX, 0), ref.random_stored(rng, N, K, ref.MX, 0)
+    (ad, asc), (wd, wsc) = stored(torch, *a), stored(torch, *w)
+    room = torch.empty((2 * far + N,), dtype=dtype_of(torch, name), device=DEV)
+    y = room.as_strided((M, N), (far, 1))
+    B.bnn_f4_gemm(ad, asc, wd, wsc, K, y, ref.MX)
+    apart = torch.empty((2 * far + 4096,), dtype=torch.uint8, device=DEV).as_strided((M, ad.shape[1]), (far, 1))
+    apart.copy_(ad)
+    z = torch.empty((M, N), dtype=y.dtype, device=DEV)
+    B.bnn_f4_gemm(apart, asc, wd, wsc, K, z, ref.MX)
+    want = product(ref.values(*a, ref.MX, K), ref.values(*w, ref.MX, K))[0]       # multiples of 1/4, held exactly by fp32
+    got = y.double().cpu().numpy()
+    assert (np.abs(got - want) <= (0 if name == "f32" else 2.0 ** -8) * np.abs(want)).all()
+    assert torch.equal(z, y)

@@ -175,3 +175,21 @@ def test_values_back(env, fmt, dtype, rows, K):
         got = y.double().cpu().numpy()
         np.testing.assert_array_equal(got[:, :K], want)
         assert (got[:, K:] == 7.0).all()
+
+
+def test_rows_further_apart_than_32_bits_hold(env):
+    torch, B = env
+    far, K = 1 << 30, 300
+    x = torch.randn((3, K), device=DEV).to(torch.bfloat16)
+    apart = torch.empty((2 * far + K,), dtype=torch.bfloat16, device=DEV).as_strided((3, K), (far, 1))
+    apart.copy_(x)
+    check(torch, B, apart, ref.NV)
+    codes = torch.empty((2 * far + 4096,), dtype=torch.uint8, device=DEV).as_strided((3, B.bnn_f4_pitch(K)), (far, 1))
+    near, scales = torch.empty((3, B.bnn_f4_pitch(K)), dtype=torch.uint8, device=DEV), torch.empty((B.bnn_f4_scale_bytes(ref.NV, 3, K),), dtype=torch.uint8, device=DEV)
+    B.bnn_f4_quantize(x, codes, scales, ref.NV)
+    B.bnn_f4_quantize(x, near, scales, ref.NV)
+    assert torch.equal(codes, near)
+    y = torch.empty((3, K), dtype=torch.bfloat16, device=DEV)
+    B.bnn_f4_dequantize(codes, scales, apart, ref.NV)
+    B.bnn_f4_dequantize(near, scales, y, ref.NV)
+    assert torch.equal(apart, y)
