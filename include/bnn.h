@@ -564,7 +564,8 @@ BNN_API int bnn_f4_gemm_grouped(const void* A, int lda, const void* a_scales, si
  *   source [T*k]  : the token of the pair at a place -- what bnn_f4_quantize takes as `source`.
  * An expert with the logit -inf (or NaN) is not chosen.  Where fewer than k are left, index and slot are -1 and the
  * weight 0; places from offsets[E] on are not written.  A NaN makes all of its token's weights NaN, and so does +inf.
- * E <= 1024, k <= 32, k <= E.  workspace: bnn_route_workspace_bytes(T, E) bytes, not used after the call's work is done.
+ * E <= 1024, k <= 32, k <= E.  workspace: bnn_route_workspace_bytes(T, E) bytes, 16-byte aligned, not used
+ * after the call's work is done.
  * Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN, BNN_ERR_UNSUPPORTED, BNN_ERR_WORKSPACE. */
 typedef enum { BNN_ROUTE_SOFTMAX = 0, BNN_ROUTE_SOFTMAX_CHOSEN = 1 } bnn_route_mode;
 BNN_API size_t bnn_route_workspace_bytes(int T, int E);

@@ -234,9 +234,10 @@ def _ptr(t, dtype=None):
 
 
 def _ld(t):
-    if t.dim() != 2 or t.stride(1) != 1:
+    stride = t.stride()
+    if len(stride) != 2 or stride[1] != 1:
         raise ValueError("expected a 2-D tensor with contiguous rows")
-    return t.stride(0)
+    return stride[0]
 
 
 def _stream():
@@ -510,7 +511,7 @@ def _dtype(t):
     return d
 
 
-def _here(*tensors):
+def _here(tensors):
     """All tensors given lie on the device that the call runs on."""
     dev = torch._C._cuda_getDevice()
     for t in tensors:
@@ -518,15 +519,14 @@ def _here(*tensors):
             raise ValueError("expected a tensor on the current CUDA device %d, got one on %s" % (dev, t.device))
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+def _refuse(what):
+    raise ValueError(what)
 
 
 def _flat(t, dtype, n, what):
     """Address of a contiguous tensor of exactly n elements."""
     if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
-        raise ValueError("%s: expected %d contiguous elements of %s, got %s of %s" % (what, n, dtype, tuple(t.shape), t.dtype))
+        _refuse("%s: expected %d contiguous elements of %s, got %s of %s" % (what, n, dtype, tuple(t.shape), t.dtype))
     return t.data_ptr()
 
 
@@ -534,8 +534,23 @@ def _codes(t, dim=2):
     """(address, pitch) of rows of codes"""
     stride = t.stride()
     if t.dtype is not torch.uint8 or len(stride) != dim or stride[-1] != 1:
-        raise ValueError("codes: expected a %d-D uint8 tensor with contiguous rows" % dim)
+        _refuse("codes: expected a %d-D uint8 tensor with contiguous rows" % dim)
     return t.data_ptr(), stride[-2]
+
+
+def _scales(t):
+    """(address, bytes) of scales or a workspace"""
+    if t.dtype is not torch.uint8 or not t.is_contiguous():
+        _refuse("scales, workspace: expected a contiguous uint8 tensor")
+    return t.data_ptr(), t.numel()
+
+
+def _groups(offsets):
+    """(address, number of groups)"""
+    if offsets is None:
+        return None, 1
+    n = offsets.numel()
+    return _flat(offsets, torch.int32, n, "offsets"), n - 1
 
 
 def bnn_f4_pitch(K) -> int:
@@ -547,23 +562,9 @@ def bnn_f4_scale_bytes(fmt, rows, K, groups=1) -> int:
     return int(lib().bnn_f4_scale_bytes(int(fmt), int(rows), int(K), int(groups)))
 
 
-def _groups(offsets):
-    """(address, number of groups)"""
-    if offsets is None:
-        return None, 1
-    n = offsets.numel()
-    return _flat(offsets, torch.int32, n, "offsets"), n - 1
-
-
-def _scales(t):
-    """(address, bytes)"""
-    n = t.numel()
-    return _flat(t, torch.uint8, n, "scales"), n
-
-
 def bnn_f4_quantize(X, codes, scales, fmt=F4_E8M0_32, source=None, offsets=None, exponent=0):
     """Rows of X (gathered by ``source``) -> ``codes`` (uint8 [rows][pitch]) and ``scales`` (uint8, bnn_f4_scale_bytes)."""
-    _here(X, codes, scales, source, offsets)
+    _here((X, codes, scales, source, offsets))
     rows = codes.shape[0]
     off, groups = _groups(offsets)
     sc, sb = _scales(scales)
@@ -575,8 +576,9 @@ def bnn_f4_quantize(X, codes, scales, fmt=F4_E8M0_32, source=None, offsets=None,
 
 def bnn_f4_dequantize(codes, scales, Y, fmt=F4_E8M0_32, offsets=None, exponent=0):
     """The values of a quantised matrix, in Y's type."""
-    _here(codes, scales, Y, offsets)
-    _need(codes.shape[0] == Y.shape[0], "codes and Y have different numbers of rows")
+    _here((codes, scales, Y, offsets))
+    if codes.shape[0] != Y.shape[0]:
+        _refuse("codes and Y have different numbers of rows")
     off, groups = _groups(offsets)
     sc, sb = _scales(scales)
     _check(lib().bnn_f4_dequantize(*_codes(codes), sc, sb, off, groups, Y.shape[0], Y.shape[1], fmt, exponent,
@@ -586,24 +588,25 @@ def bnn_f4_dequantize(codes, scales, Y, fmt=F4_E8M0_32, offsets=None, exponent=0
 
 def _f4_output(rows, n, y, act, sign_mode, scale, shift, out_bits, per):
     """(Y, dtype, ldy, epilogue)"""
-    for t in (scale, shift):
-        if t is not None:
-            _flat(t, torch.float32, per, "scale, shift")
-    if out_bits is not None:
-        _need(out_bits.shape[0] == rows, "out_bits has another number of rows")
     epi = None
     if act != ACT_NONE or scale is not None or shift is not None or out_bits is not None:
+        for t in (scale, shift):
+            if t is not None:
+                _flat(t, torch.float32, per, "scale, shift")
+        if out_bits is not None and out_bits.shape[0] != rows:
+            _refuse("out_bits has another number of rows")
         epi = C.byref(_epilogue(act, sign_mode, scale, shift, out_bits=out_bits))
     if y is None:
         return None, 0, 0, epi
-    _need(tuple(y.shape) == (rows, n), "Y: expected [%d, %d]" % (rows, n))
+    if y.shape != (rows, n):
+        _refuse("Y: expected [%d, %d]" % (rows, n))
     return y.data_ptr(), _dtype(y), _ld(y), epi
 
 
 def bnn_f4_gemm(A, a_scales, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0, act=ACT_NONE, scale=None, shift=None,
                 out_bits=None, sign_mode=SIGN_ZERO_POS):
     """Y = act(fma(scale, 2^exponent * A W^T, shift)) of two quantised matrices (codes uint8 [rows][pitch], scales)."""
-    _here(A, a_scales, W, w_scales, Y, scale, shift, out_bits)
+    _here((A, a_scales, W, w_scales, Y, scale, shift, out_bits))
     m, n = A.shape[0], W.shape[0]
     (sa, ba), (sw, bw) = _scales(a_scales), _scales(w_scales)
     y, dt, ldy, epi = _f4_output(m, n, Y, act, sign_mode, scale, shift, out_bits, n)
@@ -615,11 +618,11 @@ def bnn_f4_gemm(A, a_scales, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0,
 def bnn_f4_gemm_grouped(A, a_scales, offsets, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0, act=ACT_NONE, scale=None,
                         shift=None, out_bits=None, sign_mode=SIGN_ZERO_POS):
     """The same by groups of A's rows; ``W``: codes uint8 [groups][N][pitch], ``scale`` / ``shift``: [groups][N]."""
-    _here(A, a_scales, offsets, W, w_scales, Y, scale, shift, out_bits)
+    _here((A, a_scales, offsets, W, w_scales, Y, scale, shift, out_bits))
     off, groups = _groups(offsets)
     shape, stride = W.shape, W.stride()
-    _need(len(shape) == 3 and shape[0] == groups and (groups == 1 or stride[0] == shape[1] * stride[1]),
-          "W: expected [%d, N, pitch], the groups one behind the other" % groups)
+    if len(shape) != 3 or shape[0] != groups or (groups > 1 and stride[0] != shape[1] * stride[1]):
+        _refuse("W: expected [%d, N, pitch], the groups one behind the other" % groups)
     m, n = A.shape[0], W.shape[1]
     (sa, ba), (sw, bw) = _scales(a_scales), _scales(w_scales)
     y, dt, ldy, epi = _f4_output(m, n, Y, act, sign_mode, scale, shift, out_bits, groups * n)
@@ -634,23 +637,25 @@ def bnn_route_workspace_bytes(T, E) -> int:
 
 def bnn_route_experts(logits, index, weight, offsets, slot, source, workspace, mode=ROUTE_SOFTMAX):
     """The k best experts of each token, their weights, and the tokens sorted by expert (k = index.shape[1])."""
-    _here(logits, index, weight, offsets, slot, source, workspace)
+    _here((logits, index, weight, offsets, slot, source, workspace))
     (t, e), k = logits.shape, index.shape[1]
-    _need(index.shape[0] == t, "index has another number of tokens")
-    i32 = torch.int32
-    _check(lib().bnn_route_experts(logits.data_ptr(), _dtype(logits), t, e, _ld(logits), k, mode, _flat(index, i32, t * k, "index"),
-                                   _flat(weight, torch.float32, t * k, "weight"), _flat(offsets, i32, e + 1, "offsets"),
-                                   _flat(slot, i32, t * k, "slot"), _flat(source, i32, t * k, "source"), _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), _stream()), "bnn_route_experts")
+    if index.shape[0] != t:
+        _refuse("index has another number of tokens")
+    i32, n = torch.int32, t * k
+    _check(lib().bnn_route_experts(logits.data_ptr(), _dtype(logits), t, e, _ld(logits), k, mode, _flat(index, i32, n, "index"),
+                                   _flat(weight, torch.float32, n, "weight"), _flat(offsets, i32, e + 1, "offsets"),
+                                   _flat(slot, i32, n, "slot"), _flat(source, i32, n, "source"), *_scales(workspace),
+                                   _stream()), "bnn_route_experts")
     return index, weight, offsets, slot, source
 
 
 def bnn_combine_experts(Z, slot, weight, Y):
     """Y[t] = sum_j weight[t][j] * Z[slot[t][j]]."""
-    _here(Z, slot, weight, Y)
-    t, k = slot.shape
-    _need(Y.shape[0] == t and Y.shape[1] == Z.shape[1], "Y: expected [%d, %d]" % (t, Z.shape[1]))
-    _check(lib().bnn_combine_experts(Z.data_ptr(), _dtype(Z), Z.shape[0], _ld(Z), _flat(slot, torch.int32, t * k, "slot"),
-                                     _flat(weight, torch.float32, t * k, "weight"), t, k, Z.shape[1], Y.data_ptr(), _dtype(Y), _ld(Y),
+    _here((Z, slot, weight, Y))
+    (t, k), (rows, n) = slot.shape, Z.shape
+    if Y.shape != (t, n):
+        _refuse("Y: expected [%d, %d]" % (t, n))
+    _check(lib().bnn_combine_experts(Z.data_ptr(), _dtype(Z), rows, _ld(Z), _flat(slot, torch.int32, t * k, "slot"),
+                                     _flat(weight, torch.float32, t * k, "weight"), t, k, n, Y.data_ptr(), _dtype(Y), _ld(Y),
                                      _stream()), "bnn_combine_experts")
     return Y

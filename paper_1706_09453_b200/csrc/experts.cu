@@ -2,7 +2,7 @@
 //
 // Router: the k largest logits of a token (ties: the lowest expert), their softmax weights, and a counting sort of the T * k
 // (token, expert) pairs by expert, stable in the token: slot = offsets[expert] + how many earlier tokens chose it.  A warp takes a
-// token, its logits in registers as ordered integers; a pick is two warp reductions.  Within a block's tokens an expert has a
+// token, its logits in registers as ordered integers; a pick is a warp maximum.  Within a block's tokens an expert has a
 // bit mask of the tokens that chose it, so that a rank is a popcount and no order of atomics can change a result.  Up to
 // kOneBlock tokens one block does it all; beyond, a first kernel chooses and counts by block, and a second one adds the
 // counts of the blocks before (behind a kernel that sums them, where there are many) and places.
@@ -48,9 +48,18 @@ struct Args {
     long long ld;
     int32_t *index, *offsets, *slot, *source;
     float* weight;
-    int32_t* counts;       // [blocks][E], then [E] sums
-    int summed;            // counts hold the sums of the blocks before
+    int row;               // E rounded up to four
+    uint16_t* counts;      // [blocks][row]
+    int32_t* sums;         // [blocks + 1][E], where there are many blocks
+    int summed;
 };
+
+// exp(x) for x <= 0, within a few 2^-22.
+__device__ __forceinline__ float fast_exp(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.44269504f));
+    return r;
+}
 
 // A lane's two largest keys among those not yet taken (a bit each), and which they are; of equal keys the lowest comes first.
 template <int V>
@@ -103,7 +112,7 @@ __device__ __forceinline__ int choose(const T* x, const Args& g, int lane, float
                 // (the terms' errors, a few 2^-22 of each, do not add up in one direction)
                 float part = 0.0f;
 #pragma unroll
-                for (int v = 0; v < V; ++v) part += __expf(f[v] - first);
+                for (int v = 0; v < V; ++v) part += fast_exp(f[v] - first);
                 total = warp_sum(part);
             }
         }
@@ -133,47 +142,54 @@ __device__ __forceinline__ int choose(const T* x, const Args& g, int lane, float
     return expert;
 }
 
-// Bits of the masks -> exclusive sums over the experts in base[], by the first warp; returns the sum of all.
-__device__ __forceinline__ void scan_experts(int* base, int E, int32_t* offsets, int lane) {
-    int before = 0;
-    for (int e0 = 0; e0 < E; e0 += 32) {
-        const int e = e0 + lane, mine = e < E ? base[e] : 0;
-        int sum = mine;
+// base[e] -> the sum of all before e, by the whole block (E <= THREADS); the sums go to `offsets` as well where it is given.
+__device__ __forceinline__ void scan_experts(int* base, int E, int32_t* offsets, int lane, int warp) {
+    __shared__ int whole[WARPS];
+    const int e = threadIdx.x, mine = e < E ? base[e] : 0;
+    int sum = mine;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xFFFFFFFFu, sum, d);
-            if (lane >= d) sum += o;
-        }
-        if (e < E) {
-            base[e] = before + sum - mine;
-            if (offsets) offsets[e] = before + sum - mine;
-        }
-        before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+        if (lane >= d) sum += o;
     }
-    if (offsets && lane == 0) offsets[E] = before;
+    if (lane == 31) whole[warp] = sum;
+    __syncthreads();
+    const int before = (int)__reduce_add_sync(0xFFFFFFFFu, lane < warp ? (unsigned)whole[lane] : 0u);
+    if (e < E) {
+        base[e] = before + sum - mine;
+        if (offsets) {
+            offsets[e] = before + sum - mine;
+            if (e == E - 1) offsets[E] = before + sum;
+        }
+    }
+    __syncthreads();
 }
 
-__device__ __forceinline__ void place(const Args& g, const uint32_t* mask, const int* base, int first, int n) {
+// The places of a block's pairs; index: the block's pairs' experts (0xFFFF: none).
+__device__ __forceinline__ void place(const Args& g, const uint16_t* index, const uint32_t* mask, const int* base, int first, int n) {
     for (int i = threadIdx.x; i < n * g.k; i += THREADS) {
-        const int tl = i / g.k;
-        const size_t at = (size_t)first * g.k + i;
-        const int e = g.index[at];
+        const int tl = i / g.k, e = index[i];
         int where = -1;
-        if (e >= 0) {
+        if (e != 0xFFFF) {
             const uint32_t* m = mask + e * g.words;
             where = base[e] + __popc(m[tl >> 5] & ((1u << (tl & 31)) - 1u));
             for (int w = 0; w < tl >> 5; ++w) where += __popc(m[w]);
             g.source[where] = first + tl;
         }
-        g.slot[at] = where;
+        g.slot[(size_t)first * g.k + i] = where;
     }
 }
 
+// Shared memory of a block: masks [E][words], two numbers per expert, the experts of the block's pairs.
+__device__ __forceinline__ int* numbers_of(uint32_t* mask, const Args& g) { return reinterpret_cast<int*>(mask + g.E * g.words); }
+__device__ __forceinline__ uint16_t* pairs_of(uint32_t* mask, const Args& g) { return reinterpret_cast<uint16_t*>(mask + g.E * (g.words + 2)); }
+
 template <typename T, int V>
 __global__ void __launch_bounds__(THREADS) choose_kernel(const __grid_constant__ Args g) {
-    extern __shared__ uint32_t mask[];           // [E][words], then base[E]
+    extern __shared__ uint32_t mask[];
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint16_t* pairs = pairs_of(mask, g);
     for (int i = threadIdx.x; i < g.E * g.words; i += THREADS) mask[i] = 0u;
     pdl_wait();
     __syncthreads();
@@ -185,26 +201,26 @@ __global__ void __launch_bounds__(THREADS) choose_kernel(const __grid_constant__
             const size_t at = (size_t)(first + t) * g.k + lane;
             g.index[at] = e;
             g.weight[at] = weight;
+            pairs[t * g.k + lane] = (uint16_t)e;
             if (e >= 0) atomicOr(mask + e * g.words + (t >> 5), 1u << (t & 31));
         }
     }
     __syncthreads();
-    int* base = reinterpret_cast<int*>(mask + g.E * g.words);
-    for (int e = threadIdx.x; e < g.E; e += THREADS) {
+    int* base = numbers_of(mask, g);
+    for (int e = threadIdx.x; e < g.row; e += THREADS) {
         int c = 0;
-        for (int w = 0; w < g.words; ++w) c += __popc(mask[e * g.words + w]);
-        if (g.blocks > 1) g.counts[(size_t)blockIdx.x * g.E + e] = c;
-        else base[e] = c;
+        if (e < g.E)
+            for (int w = 0; w < g.words; ++w) c += __popc(mask[e * g.words + w]);
+        if (g.blocks > 1) g.counts[(size_t)blockIdx.x * g.row + e] = (uint16_t)c;
+        else if (e < g.E) base[e] = c;
     }
     if (g.blocks > 1) return;
     __syncthreads();
-    if (warp == 0) scan_experts(base, g.E, g.offsets, lane);
-    __syncthreads();
-    place(g, mask, base, first, n);
+    scan_experts(base, g.E, g.offsets, lane, warp);
+    place(g, pairs, mask, base, first, n);
 }
 
-// counts[b][e] -> the sum over the blocks before b, and behind them the sums over all; 32 experts a block, its warps share
-// the blocks.
+// sums[b][e]: the counts of the blocks before b, and behind them those of all; 32 experts a block, its warps share the blocks.
 __global__ void __launch_bounds__(THREADS) sum_kernel(const __grid_constant__ Args g) {
     __shared__ int part[WARPS][33];
     pdl_trigger();
@@ -213,70 +229,77 @@ __global__ void __launch_bounds__(THREADS) sum_kernel(const __grid_constant__ Ar
     const int each = ceil_div(g.blocks, WARPS), lo = min(warp * each, g.blocks), hi = min(lo + each, g.blocks);
     int sum = 0;
     if (e < g.E)
-        for (int b = lo; b < hi; ++b) sum += g.counts[(size_t)b * g.E + e];
+        for (int b = lo; b < hi; ++b) sum += g.counts[(size_t)b * g.row + e];
     part[warp][lane] = sum;
     __syncthreads();
     int before = 0;
     for (int w = 0; w < warp; ++w) before += part[w][lane];
     if (e < g.E) {
         for (int b = lo; b < hi; ++b) {
-            const int c = g.counts[(size_t)b * g.E + e];
-            g.counts[(size_t)b * g.E + e] = before;
-            before += c;
+            g.sums[(size_t)b * g.E + e] = before;
+            before += g.counts[(size_t)b * g.row + e];
         }
-        if (warp == WARPS - 1) g.counts[(size_t)g.blocks * g.E + e] = before;
+        if (warp == WARPS - 1) g.sums[(size_t)g.blocks * g.E + e] = before;
     }
 }
 
 __global__ void __launch_bounds__(THREADS) place_kernel(const __grid_constant__ Args g) {
-    extern __shared__ uint32_t mask[];           // [E][words], then base[E] and total[E]
+    extern __shared__ uint32_t mask[];
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int* base = reinterpret_cast<int*>(mask + g.E * g.words);
+    int* base = numbers_of(mask, g);
     int* total = base + g.E;
+    uint16_t* pairs = pairs_of(mask, g);
     for (int i = threadIdx.x; i < g.E * (g.words + 2); i += THREADS) mask[i] = 0u;
     pdl_wait();
     __syncthreads();
     const int first = blockIdx.x * g.chunk, n = min(g.chunk, g.T - first), mine = blockIdx.x;
     for (int i = threadIdx.x; i < n * g.k; i += THREADS) {
         const int e = g.index[(size_t)first * g.k + i], t = i / g.k;
+        pairs[i] = (uint16_t)e;
         if (e >= 0) atomicOr(mask + e * g.words + (t >> 5), 1u << (t & 31));
     }
     if (g.summed) {
         for (int e = threadIdx.x; e < g.E; e += THREADS) {
-            base[e] = g.counts[(size_t)mine * g.E + e];
-            total[e] = g.counts[(size_t)g.blocks * g.E + e];
+            base[e] = g.sums[(size_t)mine * g.E + e];
+            total[e] = g.sums[(size_t)g.blocks * g.E + e];
         }
     } else {
-        // threads of a team have an expert each, teams share the blocks; integer sums, whose order is free
-        const int width = min(THREADS, (g.E + 31) & ~31), teams = THREADS / width, team = threadIdx.x / width;
-        const int e = threadIdx.x - team * width;
-        if (e < g.E && team < teams) {
-            int before = 0, all = 0;
-            constexpr int BATCH = 16;      // loads in flight
-            for (int b0 = team; b0 < g.blocks; b0 += BATCH * teams) {
-                int c[BATCH];
+        // a thread of a team has four experts, teams share the blocks; integer sums, whose order is free
+        const int width = g.row / 4, teams = THREADS / width, team = threadIdx.x / width, e = (threadIdx.x - team * width) * 4;
+        if (team < teams) {
+            int before[4] = {0, 0, 0, 0}, all[4] = {0, 0, 0, 0};
+            for (int b0 = team; b0 < g.blocks; b0 += 10 * teams) {
+                uint2 c[10];       // loads in flight
 #pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
+                for (int i = 0; i < 10; ++i) {
                     const int b = b0 + i * teams;
-                    c[i] = b < g.blocks ? __ldcg(g.counts + (size_t)b * g.E + e) : 0;
+                    c[i] = b < g.blocks ? __ldcg(reinterpret_cast<const uint2*>(g.counts + b * g.row + e)) : make_uint2(0u, 0u);
                 }
 #pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    all += c[i];
-                    before += b0 + i * teams < mine ? c[i] : 0;
+                for (int i = 0; i < 10; ++i) {
+                    const int v[4] = {(int)(c[i].x & 0xFFFFu), (int)(c[i].x >> 16), (int)(c[i].y & 0xFFFFu), (int)(c[i].y >> 16)};
+                    const bool earlier = b0 + i * teams < mine;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        all[q] += v[q];
+                        before[q] += earlier ? v[q] : 0;
+                    }
                 }
             }
-            if (before) atomicAdd(base + e, before);
-            if (all) atomicAdd(total + e, all);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (e + q < g.E) {
+                    if (before[q]) atomicAdd(base + e + q, before[q]);
+                    if (all[q]) atomicAdd(total + e + q, all[q]);
+                }
         }
     }
     __syncthreads();
-    if (warp == 0) scan_experts(total, g.E, mine == 0 ? g.offsets : nullptr, lane);
-    __syncthreads();
+    scan_experts(total, g.E, mine == 0 ? g.offsets : nullptr, lane, warp);
     for (int e = threadIdx.x; e < g.E; e += THREADS) base[e] += total[e];
     __syncthreads();
-    place(g, mask, base, first, n);
+    place(g, pairs, mask, base, first, n);
 }
 
 struct Plan {
@@ -437,7 +460,9 @@ void (*combiner(int y_dtype, int pieces))(CombineArgs, int) {
 
 size_t route_workspace_bytes(int T, int E) {
     const Plan p = plan_of(T);
-    return p.blocks > 1 ? (size_t)(p.blocks + 1) * E * sizeof(int32_t) : 4;
+    if (p.blocks == 1) return 4;
+    const size_t counts = (size_t)p.blocks * ((E + 3) & ~3) * sizeof(uint16_t);
+    return p.blocks < kManyBlocks ? counts : counts + (size_t)(p.blocks + 1) * E * sizeof(int32_t);
 }
 
 int launch_route(const RouteArgs& a, cudaStream_t st) {
@@ -446,13 +471,15 @@ int launch_route(const RouteArgs& a, cudaStream_t st) {
     g.logits = a.logits; g.T = a.T; g.E = a.E; g.k = a.k; g.mode = a.mode; g.ld = a.ld;
     g.chunk = p.chunk; g.words = ceil_div(p.chunk, 32); g.blocks = p.blocks;
     g.index = a.index; g.offsets = a.offsets; g.slot = a.slot; g.source = a.source; g.weight = a.weight;
-    g.counts = static_cast<int32_t*>(a.workspace);
+    g.row = (a.E + 3) & ~3;
+    g.counts = static_cast<uint16_t*>(a.workspace);
+    g.sums = reinterpret_cast<int32_t*>(g.counts + (size_t)p.blocks * g.row);
     g.summed = p.blocks >= kManyBlocks;
-    const size_t smem = (size_t)a.E * (g.words + 2) * sizeof(uint32_t);
-    const int most = f4::kMaxGroups * (kMaxChunk / 32 + 2) * (int)sizeof(uint32_t);
+    auto smem_of = [](int E, int words, int pairs) { return E * (words + 2) * (int)sizeof(uint32_t) + pairs * (int)sizeof(uint16_t); };
+    const int smem = smem_of(a.E, g.words, p.chunk * a.k), most = smem_of(f4::kMaxGroups, kMaxChunk / 32, kMaxChunk * 32);
     void (*choose)(Args) = a.dtype == BNN_DTYPE_F32 ? chooser<float>(a.E) : a.dtype == BNN_DTYPE_F16 ? chooser<__half>(a.E) : chooser<__nv_bfloat16>(a.E);
     if (!ensure_dynamic_smem(reinterpret_cast<const void*>(choose), most) ||
-        !ensure_dynamic_smem(reinterpret_cast<const void*>(place_kernel), most))
+        (p.blocks > 1 && !ensure_dynamic_smem(reinterpret_cast<const void*>(place_kernel), most)))
         return BNN_ERR_CUDA;
     if (launch_pdl(choose, dim3(p.blocks), dim3(THREADS), smem, st, g) != cudaSuccess) return BNN_ERR_CUDA;
     if (p.blocks > 1) {

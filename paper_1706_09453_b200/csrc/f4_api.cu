@@ -146,7 +146,7 @@ int bnn_route_experts(const void* logits, int dtype, int T, int E, int ld, int k
     if (!known_dtype(dtype) || (mode != BNN_ROUTE_SOFTMAX && mode != BNN_ROUTE_SOFTMAX_CHOSEN)) return BNN_ERR_UNSUPPORTED;
     if (T < 1 || E < 1 || E > f4::kMaxGroups || ld < E || k < 1 || k > E || k > kMaxChoices || T > 0x7FFFFFFF / k) return BNN_ERR_SHAPE;
     if (!aligned_to(logits, size_of(dtype)) || !aligned_to(index, 4) || !aligned_to(weight, 4) || !aligned_to(offsets, 4) ||
-        !aligned_to(slot, 4) || !aligned_to(source, 4) || !aligned_to(workspace, 4))
+        !aligned_to(slot, 4) || !aligned_to(source, 4) || !aligned16(workspace))
         return BNN_ERR_ALIGN;
     if (!workspace || workspace_bytes < route_workspace_bytes(T, E)) return BNN_ERR_WORKSPACE;
     RouteArgs a{};

@@ -70,6 +70,19 @@ def test_ties_and_masked_experts(env, T, E, k):
     check_route(torch, B, lowest, k)
 
 
+@pytest.mark.parametrize("E", [40, 256, 900])
+def test_logits_that_differ_in_their_last_bits(env, E):
+    """fp32 steps apart, on both sides of zero, at and around the k-th place."""
+    torch, B = env
+    rng = np.random.default_rng(E)
+    T, k = 300, 6
+    base = rng.choice(np.array([1.0, -1.0, 3.5e-3, -7.25e4], dtype=np.float32), (T, 1))
+    x = (base.view(np.int32) + rng.integers(0, 40, (T, E), dtype=np.int32)).view(np.float32)
+    check_route(torch, B, torch.as_tensor(x, device=DEV), k)
+    h = (rng.choice(np.array([1.0, -1.0, 0.01, -300.0, 1e-6], dtype=np.float16), (T, 1)).view(np.int16) + rng.integers(0, 60, (T, E), dtype=np.int16)).view(np.float16)
+    check_route(torch, B, torch.as_tensor(h, device=DEV), k)
+
+
 def test_nan_and_infinity(env):
     torch, B = env
     x = torch.randn((6, 20), device=DEV)
