@@ -12,6 +12,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "f4.cuh"
 
 namespace bnn {
@@ -53,7 +55,7 @@ __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
 }
 
 // Eight numbers -> eight codes, the first in the lowest nibble: to the nearest, ties to even, beyond 6 becomes 6.
-__device__ __forceinline__ uint32_t to_codes(const float (&v)[8]) {
+__device__ __forceinline__ uint32_t to_codes(const float* v) {
     uint32_t r;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
@@ -93,139 +95,150 @@ __device__ __forceinline__ bool locate(const int32_t* offsets, int groups, int r
     return true;
 }
 
-// Largest magnitude of eight elements as the bits of an fp32 number (NaNs are above all others).
-__device__ __forceinline__ uint32_t magnitude(const float (&v)[8]) {
+// Sixteen consecutive elements from p (32-byte aligned) by 32-byte loads.
+__device__ __forceinline__ void ldg32(const void* p, uint32_t (&w)[8]) {
+    asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+}
+template <typename T> struct Sixteen {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const T* p) { ldg32(p, w); }
+    __device__ __forceinline__ void values(float (&v)[16]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            T h[2];
+            memcpy(h, &w[i], 4);
+            v[2 * i] = to_f32(h[0]);
+            v[2 * i + 1] = to_f32(h[1]);
+        }
+    }
+    // the largest magnitude as the bits of an fp32 number, two elements at a time
+    __device__ __forceinline__ uint32_t magnitude() const {
+        uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+        m = max(m & 0xFFFFu, m >> 16);
+        return std::is_same<T, __half>::value ? __float_as_uint(__half2float(__ushort_as_half((unsigned short)m))) : m << 16;
+    }
+};
+template <> struct Sixteen<float> {
+    uint32_t w[16];
+    __device__ __forceinline__ void load(const float* p) {
+        ldg32(p, reinterpret_cast<uint32_t(&)[8]>(w[0]));
+        ldg32(p + 8, reinterpret_cast<uint32_t(&)[8]>(w[8]));
+    }
+    __device__ __forceinline__ void values(float (&v)[16]) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(w[i]);
+    }
+    __device__ __forceinline__ uint32_t magnitude() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
+        return m;
+    }
+};
+
+// Largest magnitude of N elements as the bits of an fp32 number (NaNs are above all others).
+template <int N>
+__device__ __forceinline__ uint32_t magnitude(const float (&v)[N]) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
     return m;
 }
-// The same from eight 16-bit elements as they were loaded, two at a time.
-__device__ __forceinline__ uint32_t magnitude2(const uint4& w) {
-    const uint32_t keep = 0x7FFF7FFFu;
-    const uint32_t m = __vmaxu2(__vmaxu2(w.x & keep, w.y & keep), __vmaxu2(w.z & keep, w.w & keep));
-    return max(m & 0xFFFFu, m >> 16);
-}
-__device__ __forceinline__ uint32_t widen_magnitude(uint32_t m, __nv_bfloat16) { return m << 16; }
-__device__ __forceinline__ uint32_t widen_magnitude(uint32_t m, __half) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m))); }
 
-// One block's share of a lane: eight elements and the block's largest magnitude -> codes, and the scale's byte.
-template <bool MX>
-__device__ __forceinline__ uint32_t to_block(float (&v)[8], uint32_t most, uint32_t* scale) {
+// One block's share of a lane: N elements and the block's largest magnitude -> codes, eight to a word, and the scale's byte.
+template <bool MX, int N>
+__device__ __forceinline__ void to_block(float (&v)[N], uint32_t most, uint32_t (&codes)[N / 8], uint32_t* scale) {
     const bool finite = most < 0x7F800000u;
-    uint32_t byte, codes;
+    uint32_t byte;
     if (MX) {
         byte = max(most >> 23, 2u) - 2u;
         const float inverse = __uint_as_float((254u - byte) << 23);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= inverse;
-        codes = to_codes(v);
+        for (int i = 0; i < N; ++i) v[i] *= inverse;
     } else {
         byte = to_e4m3(__fdiv_rn(__uint_as_float(most), 6.0f));
         const float s = from_e4m3(byte), inverse = __frcp_rn(s);
         // The quotient to the nearest from the rounded reciprocal (Markstein, IBM J. Res. Dev. 34, 1990): the remainder
         // is exact in a fused multiply-add, and one correction rounds as a division does.  (It makes +0 of -0.)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             const float q = v[i] * inverse;
             v[i] = copysignf(byte ? __fmaf_rn(__fmaf_rn(-q, s, v[i]), inverse, q) : 0.0f, v[i]);
         }
-        codes = to_codes(v);
+    }
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) {
+        codes[i] = to_codes(&v[8 * i]);
+        if (!finite) codes[i] = 0u;
     }
     *scale = finite ? byte : MX ? 0xFFu : 0x7Fu;
-    return finite ? codes : 0u;
 }
 
-template <bool MX>
-__device__ __forceinline__ uint32_t block_max(uint32_t m) {
-    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-    if (MX) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-    return m;
-}
-
-// A warp: UNROLL segments of 256 elements of a row.
-template <typename T, bool MX, bool VEC, int UNROLL>
-__global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const __grid_constant__ F4QuantArgs g, int turns, long long items) {
+// A warp: SEGMENT elements of a row; the warps of a block: rows one behind the other.  WIDE (32-byte aligned rows): a lane has 16
+// consecutive elements twice where all of the segment exists, which is half of an e8m0 block or a whole e4m3 block; else 8 and
+// tests on the way.
+constexpr int SEGMENT = 1024;
+template <typename T, bool MX, bool VEC, bool WIDE>
+__global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const __grid_constant__ F4QuantArgs g, int segment) {
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31;
-    const long long item = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
-    if (item >= items) return;
-    const int row = (int)(item / turns), first = (int)(item - (long long)row * turns) * UNROLL * 256;
+    const int row = blockIdx.x * WARPS + (threadIdx.x >> 5), first = blockIdx.y * segment;
+    if (row >= g.rows) return;
     const int src = g.source ? __ldg(g.source + row) : row;
-    const T* x = static_cast<const T*>(g.X) + (long long)src * g.ldx + first + lane * 8;
+    const T* x = static_cast<const T*>(g.X) + (long long)src * g.ldx + first;
     const bool there = !g.source || (src >= 0 && src < g.src_rows);
-    constexpr int LANES = MX ? 4 : 2;                     // lanes of a block
-    const int k0 = first + lane * 8, kt = f4::scale_tiles(g.format, g.K);
+    const int kt = f4::scale_tiles(g.format, g.K);
+    constexpr int BLOCK = MX ? 32 : 16;
     int tile, local;
-    // a lane's blocks are 256 / (8 LANES) apart, as many as fill 256 / (32 LANES) tiles
-    constexpr int TILES = 256 / (32 * LANES);
-    const int block = k0 / (8 * LANES);
-    if (VEC && there && first + UNROLL * 256 <= g.K) {
-        // all of it exists: no test on the way
-        if constexpr (sizeof(T) == 2) {
-            uint4 raw[UNROLL];
+    if (WIDE && there && first + SEGMENT <= g.K) {       // (segment == SEGMENT)
+        Sixteen<T> raw[2];
+        raw[0].load(x + lane * 16);
+        raw[1].load(x + 512 + lane * 16);
+        if (!locate(g.offsets, g.groups, row, lane, &tile, &local)) return;
+        const int k0 = first + lane * 16, block = k0 / BLOCK;
+        uint8_t* codes = g.codes + (size_t)row * g.ldc + (k0 >> 1);
+        uint8_t* scales = g.scales + scale_place(tile, kt, block >> 2, local) + (block & 3);
+        const bool writer = !MX || !(lane & 1);
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) raw[u] = __ldg(reinterpret_cast<const uint4*>(x + u * 256));
-            if (!locate(g.offsets, g.groups, row, lane, &tile, &local)) return;
-            uint8_t* codes = g.codes + (size_t)row * g.ldc + (k0 >> 1);
-            uint8_t* scales = g.scales + scale_place(tile, kt, block >> 2, local) + (block & 3);
+        for (int u = 0; u < 2; ++u) {
+            float v[16];
+            raw[u].values(v);
+            uint32_t most;
+            if (g.factor == 1.0f) {
+                most = raw[u].magnitude();
+            } else {
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                float v[8];
-                const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    T h[2];
-                    memcpy(h, &w[i], 4);
-                    v[2 * i] = to_f32(h[0]);
-                    v[2 * i + 1] = to_f32(h[1]);
-                }
-                uint32_t most;
-                if (g.factor == 1.0f) {
-                    most = widen_magnitude(block_max<MX>(magnitude2(raw[u])), T());
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] *= g.factor;
-                    most = block_max<MX>(magnitude(v));
-                }
-                uint32_t byte;
-                *reinterpret_cast<uint32_t*>(codes + u * 128) = to_block<MX>(v, most, &byte);
-                if (lane % LANES == 0) scales[u * TILES * 512] = (uint8_t)byte;
+                for (int i = 0; i < 16; ++i) v[i] *= g.factor;
+                most = magnitude(v);
             }
-        } else {
-            float v[UNROLL][8];
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u) load8<true>(x + u * 256, 8, v[u]);
-            if (!locate(g.offsets, g.groups, row, lane, &tile, &local)) return;
-            uint8_t* codes = g.codes + (size_t)row * g.ldc + (k0 >> 1);
-            uint8_t* scales = g.scales + scale_place(tile, kt, block >> 2, local) + (block & 3);
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[u][i] *= g.factor;
-                uint32_t byte;
-                const uint32_t most = block_max<MX>(magnitude(v[u]));
-                *reinterpret_cast<uint32_t*>(codes + u * 128) = to_block<MX>(v[u], most, &byte);
-                if (lane % LANES == 0) scales[u * TILES * 512] = (uint8_t)byte;
-            }
+            if (MX) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+            uint32_t c[2], byte;
+            to_block<MX>(v, most, c, &byte);
+            *reinterpret_cast<uint2*>(codes + u * 256) = make_uint2(c[0], c[1]);
+            if (writer) scales[u * (128 / BLOCK) * 512] = (uint8_t)byte;
         }
         return;
     }
     if (!locate(g.offsets, g.groups, row, lane, &tile, &local)) return;
     const int bytes = f4::code_bytes(g.K);
 #pragma unroll 1
-    for (int u = 0; u < UNROLL; ++u) {
-        const int k = k0 + u * 256;
+    for (int s = 0; s < segment; s += 256) {
+        const int k = first + s + lane * 8, block = k / BLOCK;
         float v[8];
-        load8<VEC>(x + u * 256, there ? g.K - k : 0, v);
+        load8<VEC>(x + s + lane * 8, there ? g.K - k : 0, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= g.factor;
-        uint32_t byte;
-        const uint32_t codes = to_block<MX>(v, block_max<MX>(magnitude(v)), &byte);
-        if (k >> 1 < bytes) *reinterpret_cast<uint32_t*>(g.codes + (size_t)row * g.ldc + (k >> 1)) = codes;
-        const int b = block + u * TILES * 4;
-        if (lane % LANES == 0 && b >> 2 < kt) g.scales[scale_place(tile, kt, b >> 2, local) + (b & 3)] = k < g.K ? (uint8_t)byte : (uint8_t)0;
+        uint32_t most = magnitude(v);
+        most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+        if (MX) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+        uint32_t c[1], byte;
+        to_block<MX>(v, most, c, &byte);
+        if (k >> 1 < bytes) *reinterpret_cast<uint32_t*>(g.codes + (size_t)row * g.ldc + (k >> 1)) = c[0];
+        if (k % BLOCK == 0 && block >> 2 < kt) g.scales[scale_place(tile, kt, block >> 2, local) + (block & 3)] = k < g.K ? (uint8_t)byte : (uint8_t)0;
     }
 }
 
@@ -236,6 +249,27 @@ __device__ __forceinline__ float2 from_codes(uint32_t pair) {
     __half2 p;
     memcpy(&p, &h, 4);
     return __half22float2(p);
+}
+
+// Four codes (16 bits) -> four bf16, two to a word.  The bytes of the eight magnitudes come from tables of eight bytes by byte permutation,
+// whose selector is the code itself; a selector's bit 3 (the sign) makes it replicate the byte's top bit, which tells 0x80 from 0xFF.
+__device__ __forceinline__ void to_bf16(uint32_t codes, uint32_t* first, uint32_t* second) {
+    const uint32_t mag = codes & 0x7777u;
+    const uint32_t lo = __byte_perm(0xC0800000u, 0xC0804000u, mag);     // 0 .5 1 1.5 | 2 3 4 6: 0000 3F00 3F80 3FC0 4000 4040 4080 40C0
+    uint32_t hi = __byte_perm(0x3F3F3F00u, 0x40404040u, mag);
+    uint32_t sign;
+    asm("prmt.b32 %0, %1, %1, %2;" : "=r"(sign) : "r"(0x80808080u), "r"(codes));
+    hi |= (sign << 1) & 0x80808080u;
+    *first = __byte_perm(lo, hi, 0x5140);
+    *second = __byte_perm(lo, hi, 0x7362);
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    __nv_bfloat162 x, y;
+    memcpy(&x, &a, 4);
+    memcpy(&y, &b, 4);
+    x = __hmul2(x, y);
+    memcpy(&a, &x, 4);
+    return a;
 }
 
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
@@ -273,13 +307,12 @@ __device__ __forceinline__ void store8(T* p, int n, const float (&v)[8]) {
 }
 
 template <typename T, bool MX, bool VEC, int UNROLL>
-__global__ void __launch_bounds__(WARPS * 32) dequantize_kernel(const __grid_constant__ F4DequantArgs g, int turns, long long items) {
+__global__ void __launch_bounds__(WARPS * 32) dequantize_kernel(const __grid_constant__ F4DequantArgs g) {
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31;
-    const long long item = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
-    if (item >= items) return;
-    const int row = (int)(item / turns), first = (int)(item % turns) * UNROLL * 256;
+    const int row = blockIdx.x * WARPS + (threadIdx.x >> 5), first = blockIdx.y * UNROLL * 256;
+    if (row >= g.rows) return;
     const int kt = f4::scale_tiles(g.format, g.K);
     uint32_t codes[UNROLL];
 #pragma unroll
@@ -301,62 +334,83 @@ __global__ void __launch_bounds__(WARPS * 32) dequantize_kernel(const __grid_con
         const int n = g.K - k0 - u * 256;
         if (n <= 0) continue;
         const float s = MX ? from_e8m0(byte[u]) : from_e4m3(byte[u] & 0x7Fu);
+        if constexpr (VEC && sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value) {
+            if (n >= 8) {
+                // a code times a scale has at most six bits: exact in bf16, whose exponents are those of fp32
+                uint32_t w[4];
+                to_bf16(codes[u] & 0xFFFFu, &w[0], &w[1]);
+                to_bf16(codes[u] >> 16, &w[2], &w[3]);
+                // (the factor first: that product neither overflows nor underflows, so that all is rounded once)
+                if (g.factor != 1.0f) {
+                    const uint32_t f2 = (__float_as_uint(g.factor) >> 16) * 0x10001u;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = mul_bf16x2(w[i], f2);
+                }
+                const uint32_t s2 = (__float_as_uint(s) >> 16) * 0x10001u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = mul_bf16x2(w[i], s2);
+                *reinterpret_cast<uint4*>(y + u * 256) = make_uint4(w[0], w[1], w[2], w[3]);
+                continue;
+            }
+        }
         float v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 p = from_codes(codes[u] >> (8 * i));
-            v[2 * i] = p.x * s;
-            v[2 * i + 1] = p.y * s;
-        }
-        if (g.factor != 1.0f) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= g.factor;
+            v[2 * i] = p.x * g.factor * s;
+            v[2 * i + 1] = p.y * g.factor * s;
         }
         store8<VEC>(y + u * 256, n, v);
     }
 }
 
-template <typename A>
-using Kernel = void (*)(A, int, long long);
-
-template <typename T, bool VEC, int U>
-Kernel<F4QuantArgs> quantizer(int format) {
-    return format == BNN_F4_E8M0_32 ? quantize_kernel<T, true, VEC, U> : quantize_kernel<T, false, VEC, U>;
+template <typename T, bool VEC, bool WIDE>
+void (*quantizer(int format))(F4QuantArgs, int) {
+    return format == BNN_F4_E8M0_32 ? quantize_kernel<T, true, VEC, WIDE> : quantize_kernel<T, false, VEC, WIDE>;
+}
+template <typename T>
+void (*quantizer(int format, bool vec, bool wide))(F4QuantArgs, int) {
+    return wide ? quantizer<T, true, true>(format) : vec ? quantizer<T, true, false>(format) : quantizer<T, false, false>(format);
 }
 template <typename T, bool VEC, int U>
-Kernel<F4DequantArgs> dequantizer(int format) {
+void (*dequantizer(int format))(F4DequantArgs) {
     return format == BNN_F4_E8M0_32 ? dequantize_kernel<T, true, VEC, U> : dequantize_kernel<T, false, VEC, U>;
 }
 template <typename T>
-Kernel<F4QuantArgs> pick(const F4QuantArgs& a, bool vec, bool many) {
-    if (many) return vec ? quantizer<T, true, 4>(a.format) : quantizer<T, false, 4>(a.format);
-    return vec ? quantizer<T, true, 1>(a.format) : quantizer<T, false, 1>(a.format);
-}
-template <typename T>
-Kernel<F4DequantArgs> pick(const F4DequantArgs& a, bool vec, bool many) {
-    if (many) return vec ? dequantizer<T, true, 4>(a.format) : dequantizer<T, false, 4>(a.format);
-    return vec ? dequantizer<T, true, 1>(a.format) : dequantizer<T, false, 1>(a.format);
+void (*dequantizer(int format, bool vec, bool many))(F4DequantArgs) {
+    if (many) return vec ? dequantizer<T, true, 4>(format) : dequantizer<T, false, 4>(format);
+    return vec ? dequantizer<T, true, 1>(format) : dequantizer<T, false, 1>(format);
 }
 
-template <typename A>
-int launch(const A& a, const void* real, int dtype, int ld, cudaStream_t st) {
-    const int size = dtype == BNN_DTYPE_F32 ? 4 : 2;
-    const bool vec = aligned16(real) && ((long long)ld * size) % 16 == 0;
-    const int segments = ceil_div(a.K, 256);
-    // Four segments a warp where there is enough for every SM's warps, so that a lane has four loads in flight.
-    const bool many = (long long)a.rows * segments >= 4LL * 148 * 64 && segments >= 4;
-    const int turns = ceil_div(segments, many ? 4 : 1);
-    const long long items = (long long)a.rows * turns, grid = (items + WARPS - 1) / WARPS;
-    if (grid > 0x7FFFFFFF) return BNN_ERR_SHAPE;
-    Kernel<A> kern = dtype == BNN_DTYPE_F32 ? pick<float>(a, vec, many)
-                   : dtype == BNN_DTYPE_F16 ? pick<__half>(a, vec, many) : pick<__nv_bfloat16>(a, vec, many);
-    if (launch_pdl(kern, dim3((unsigned)grid), dim3(WARPS * 32), 0, st, a, turns, items) != cudaSuccess) return BNN_ERR_CUDA;
-    return launch_status();
+bool rows_aligned(const void* p, int dtype, int ld, int to) {
+    return reinterpret_cast<uintptr_t>(p) % to == 0 && ((long long)ld * (dtype == BNN_DTYPE_F32 ? 4 : 2)) % to == 0;
 }
+// 1024 elements a warp where there is enough of that for every SM's warps (or too much for the grid's height), else 256.
+bool long_segments(int rows, int K) {
+    const int segments = ceil_div(K, 256);
+    return segments > 65535 || ((long long)rows * segments >= 4LL * 148 * 64 && segments >= 4);
+}
+// A warp's row and its columns are its block's coordinates (a division by the segments was a quarter of the instructions).
+dim3 grid_of(int rows, int K, int segment) { return dim3(ceil_div(rows, WARPS), ceil_div(K, segment)); }
 
 }  // namespace
 
-int launch_f4_quantize(const F4QuantArgs& a, cudaStream_t st) { return launch(a, a.X, a.dtype, a.ldx, st); }
-int launch_f4_dequantize(const F4DequantArgs& a, cudaStream_t st) { return launch(a, a.Y, a.dtype, a.ldy, st); }
+int launch_f4_quantize(const F4QuantArgs& a, cudaStream_t st) {
+    const int segment = long_segments(a.rows, a.K) ? SEGMENT : 256;
+    const bool vec = rows_aligned(a.X, a.dtype, a.ldx, 16), wide = segment == SEGMENT && rows_aligned(a.X, a.dtype, a.ldx, 32);
+    auto kern = a.dtype == BNN_DTYPE_F32 ? quantizer<float>(a.format, vec, wide)
+              : a.dtype == BNN_DTYPE_F16 ? quantizer<__half>(a.format, vec, wide) : quantizer<__nv_bfloat16>(a.format, vec, wide);
+    // (a segment always takes all scale tiles that it begins, also where K ends inside the last one)
+    if (launch_pdl(kern, grid_of(a.rows, a.K, segment), dim3(WARPS * 32), 0, st, a, segment) != cudaSuccess) return BNN_ERR_CUDA;
+    return launch_status();
+}
+
+int launch_f4_dequantize(const F4DequantArgs& a, cudaStream_t st) {
+    const bool many = long_segments(a.rows, a.K), vec = rows_aligned(a.Y, a.dtype, a.ldy, 16);
+    auto kern = a.dtype == BNN_DTYPE_F32 ? dequantizer<float>(a.format, vec, many)
+              : a.dtype == BNN_DTYPE_F16 ? dequantizer<__half>(a.format, vec, many) : dequantizer<__nv_bfloat16>(a.format, vec, many);
+    if (launch_pdl(kern, grid_of(a.rows, a.K, many ? 1024 : 256), dim3(WARPS * 32), 0, st, a) != cudaSuccess) return BNN_ERR_CUDA;
+    return launch_status();
+}
 
 }  // namespace bnn

@@ -193,3 +193,19 @@ def test_rows_further_apart_than_32_bits_hold(env):
     B.bnn_f4_dequantize(codes, scales, apart, ref.NV)
     B.bnn_f4_dequantize(near, scales, y, ref.NV)
     assert torch.equal(apart, y)
+
+
+@pytest.mark.parametrize("fmt", [ref.MX, ref.NV])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("exponent", [0, -64, 64])
+def test_every_scale_back(env, fmt, dtype, exponent):
+    """All codes with all scale bytes; what lies below the type's smallest normal number is rounded to its subnormal ones."""
+    torch, B = env
+    K, dt = 128, dtype_of(torch, dtype)
+    code = np.tile(np.arange(16, dtype=np.uint8), (256 if fmt == ref.MX else 128, K // 16))
+    rows = code.shape[0]
+    byte = np.tile(np.arange(rows, dtype=np.uint8)[:, None], (1, 4 * ref.scale_tiles(fmt, K)))
+    y = torch.empty((rows, K), dtype=dt, device=DEV)
+    B.bnn_f4_dequantize(torch.as_tensor(ref.pack(code), device=DEV), torch.as_tensor(ref.store_scales(byte, None, 1), device=DEV), y, fmt, exponent=exponent)
+    want = torch.as_tensor(ref.values(code, byte, fmt, K) * 2.0 ** exponent).to(dt).double().numpy()
+    np.testing.assert_array_equal(y.double().cpu().numpy(), want)
