@@ -43,7 +43,7 @@ int gemm_checked(const void* a, int lda, const void* a_scales, size_t a_scale_by
     if (int rc = check_groups(offsets, groups)) return rc;
     const long long units = (long long)groups * N;
     if (units > 0x7FFFFFFF - 256 || M > 0x7FFFFFFF - 512) return BNN_ERR_SHAPE;
-    if (((long long)M / 32 + groups) * ceil_div(N, 128) > 0x7FFFFFFF) return BNN_ERR_SHAPE;
+    if (((long long)M / 32 + groups) * ceil_div(N, 128) > 0x7FFF0000) return BNN_ERR_SHAPE;
     if (int rc = check_f4(a, lda, a_scales, a_scale_bytes, format, M, groups, K)) return rc;
     if (int rc = check_f4(w, ldw, w_scales, w_scale_bytes, format, units, groups, K)) return rc;
     F4GemmArgs g{};

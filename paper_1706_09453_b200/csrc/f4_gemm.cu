@@ -28,8 +28,10 @@ constexpr int TMEM_COLS = 512, SF_COL = 480;
 constexpr int PANEL = 8;
 constexpr int SMEM_LIMIT = 232448, MAX_STAGES = 10;
 constexpr int OUT_CHUNK = 32 * 64;       // a warp's 32 rows x 32 units of 16 bits on their way out
+constexpr int PAIR_ROWS = 256;           // rows of a pair's tile
+constexpr int MAX_SPLIT = 4;             // CTAs that share the K of a tile
 
-template <bool MX, bool PAIR, int TN>
+template <bool MX, bool PAIR, int TN, bool SPLIT>
 struct Shape {
     static constexpr int KATOMS = MX ? 2 : 4;                     // scale tiles (four blocks of K) of a stage
     static constexpr int B_ROWS = PAIR ? TN / 2 : TN;             // rows of activations in this CTA's shared memory
@@ -38,7 +40,7 @@ struct Shape {
     static constexpr int SFA_BYTES = KATOMS * 512, SFB_BYTES = ROW_TILES * KATOMS * 512;
     static constexpr int STAGE = A_BYTES + B_BYTES + SFA_BYTES + SFB_BYTES;
     static constexpr int CONTROL = 512 + (f4::kMaxGroups + 1) * 8;
-    static constexpr int OUT_BYTES = EPI_WARPS * OUT_CHUNK;
+    static constexpr int OUT_BYTES = SPLIT ? TN * BM * 4 : EPI_WARPS * OUT_CHUNK;
     static constexpr int FIT = (SMEM_LIMIT - 1024 - CONTROL - OUT_BYTES) / STAGE;
     static constexpr int STAGES = FIT > MAX_STAGES ? MAX_STAGES : FIT;
     static constexpr int SMEM = STAGES * STAGE + OUT_BYTES + CONTROL + 1024;
@@ -57,7 +59,7 @@ struct Args {
     float factor;
     const float* scale;
     const float* shift;
-    int act, sign_mode, box;
+    int act, sign_mode, box, split;
     void* Y;
     int dtype, pieces;
     long long ldy;
@@ -79,27 +81,39 @@ static_assert(sizeof(Control) <= 512 + (f4::kMaxGroups + 1) * 8, "");
 
 struct Tile {
     int g, row0, n, unit0, a_tile;
+    uint32_t sf_off;        // columns of the scale tile before the first row's
 };
 
-// Tile number w: panels of PANEL unit tiles, in which the units run fastest, so that the tiles that run at the same time
-// are about as many unit tiles as row tiles and share both operands' reads.
-template <int TN>
-__device__ __forceinline__ Tile tile_at(const Control* ctl, const Args& g, int w, int unit_tiles, int unit_step) {
-    const int rows = ctl->tiles[g.groups], panel = w / (rows * PANEL), in = w - panel * rows * PANEL;
-    const int wide = min(PANEL, unit_tiles - panel * PANEL), j = in / wide;
-    Tile t;
-    t.unit0 = (panel * PANEL + in - j * wide) * unit_step;
-    int lo = 0, hi = g.groups;               // the last group whose tiles start at or before j
+// The group of which row tile j (of all groups, counted one behind the other) is one: the last whose tiles start at or before it.
+__device__ __forceinline__ int group_of(const Control* ctl, int groups, int j) {
+    int lo = 0, hi = groups;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (ctl->tiles[mid] <= j) lo = mid; else hi = mid;
     }
-    t.g = lo;
-    const int off = (j - ctl->tiles[lo]) * TN, begin = ctl->first[lo];
+    return lo;
+}
+template <int TN>
+__device__ __forceinline__ Tile make_tile(const Control* ctl, int group, int row_tile, int unit0) {
+    Tile t;
+    t.g = group;
+    t.unit0 = unit0;
+    const int off = row_tile * TN, begin = ctl->first[group];
     t.row0 = begin + off;
-    t.n = min(TN, ctl->first[lo + 1] - t.row0);
-    t.a_tile = begin / 128 + lo + off / 128;
+    t.n = min(TN, ctl->first[group + 1] - t.row0);
+    t.a_tile = begin / 128 + group + off / 128;
+    t.sf_off = (off & 127) >> 5;
     return t;
+}
+
+// Tile number w: panels of PANEL unit tiles, in which the units run fastest, so that the tiles that run at the same time
+// are about as many unit tiles as row tiles and share both operands' reads.  (Consecutive tiles for a CTA, whose weights then stay
+// in shared memory, are slower: 8192 x 4096 x 8192 113 us instead of 108, 32 groups 89 instead of 83.)
+template <int TN>
+__device__ __forceinline__ Tile tile_at(const Control* ctl, const Args& g, int w, int unit_tiles, int unit_step) {
+    const int rows = ctl->tiles[g.groups], panel = w / (rows * PANEL), in = w - panel * rows * PANEL;
+    const int wide = min(PANEL, unit_tiles - panel * PANEL), j = in / wide, group = group_of(ctl, g.groups, j);
+    return make_tile<TN>(ctl, group, j - ctl->tiles[group], (panel * PANEL + in - j * wide) * unit_step);
 }
 
 template <bool PAIR>
@@ -126,7 +140,6 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16) {
 
 // Where a warp's chunk of 32 units x 32 rows goes: the first unit's address in the first row, how many units and rows exist.
 struct Chunk {
-    float factor;
     long long ldy;
     int units, rows;
 };
@@ -142,16 +155,17 @@ __device__ __forceinline__ void store_units(T* y, const Chunk& c, uint32_t taddr
     y += lane;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-        if (i < c.rows) put(y, activate<ACT>(fmaf(scale, __uint_as_float(acc[i]) * c.factor, shift)));
+        if (i < c.rows) put(y, activate<ACT>(fmaf(scale, __uint_as_float(acc[i]), shift)));
         y += c.ldy;
     }
 }
 
 // 16 bits, rows of Y on 16-byte boundaries: the accumulator comes in the layout of an MMA's result, goes to shared memory
-// transposed (row by row, 64 bytes each) and from there in pieces of 16 bytes: 4 stores to a chunk instead of 32 (8192 x 1024 x
-// 8192: 46 us instead of 88).
-// out: this warp's chunk of shared memory; piece p of row r lies at r * 64 + 16 * (p ^ (r / 2) % 4), so that neither side meets itself
-// in a bank.  scale, shift: of units lane / 4 + 8 i.  `next`: the chunk to load into acc once this one's values are taken.
+// transposed and from there, in pieces of 16 bytes, out in rows of 256 bytes: the four warps that hold the tile's 128 units share a
+// chunk of 32 rows.  (8192 x 1024 x 8192: element by element 88 us, a warp's rows of 64 bytes 46 us.)
+// out: the four warps' 32 x 256 bytes; piece p of row r lies at r * 256 + 16 * (p ^ r % 8), so that neither side meets itself in a
+// bank.  scale, shift: of units lane / 4 + 8 i.  c.units: from the tile's first unit on.  `next`: the chunk to load into acc once
+// this one's values are taken.
 struct Frag {
     uint32_t lo[16], hi[16];
     __device__ __forceinline__ void load(uint32_t taddr) {
@@ -160,10 +174,10 @@ struct Frag {
     }
 };
 template <int ACT, typename T>
-__device__ __forceinline__ void store_pieces(T* y, const Chunk& c, Frag& acc, int lane, uint32_t out, const float (&scale)[4],
-                                             const float (&shift)[4], bool more, uint32_t next) {
+__device__ __forceinline__ void store_pieces(T* y, const Chunk& c, Frag& acc, int half, int quarter, int lane, uint32_t out,
+                                             const float (&scale)[4], const float (&shift)[4], bool more, uint32_t next) {
     uint32_t v[4][4];
-    auto val = [&](uint32_t a, int i) { return activate<ACT>(fmaf(scale[i], __uint_as_float(a) * c.factor, shift[i])); };
+    auto val = [&](uint32_t a, int i) { return activate<ACT>(fmaf(scale[i], __uint_as_float(a), shift[i])); };
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         v[j][0] = pack2(val(acc.lo[4 * j], 0), val(acc.lo[4 * j + 1], 0), T());
@@ -175,14 +189,14 @@ __device__ __forceinline__ void store_pieces(T* y, const Chunk& c, Frag& acc, in
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int row = 8 * j + (lane & 7);
-        stmatrix4_trans(out + row * 64 + (((lane >> 3) ^ (row >> 1)) & 3) * 16, v[j][0], v[j][1], v[j][2], v[j][3]);
+        stmatrix4_trans(out + row * 256 + ((quarter * 4 + (lane >> 3)) ^ (row & 7)) * 16, v[j][0], v[j][1], v[j][2], v[j][3]);
     }
-    __syncwarp();
-    const int piece = lane & 3, units = c.units - piece * 8;
+    bar_sync_128(4 + half);
+    const int piece = lane & 15, units = c.units - piece * 8;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int row = 8 * j + (lane >> 2);
-        const uint4 w = lds128u(out + row * 64 + ((piece ^ (row >> 1)) & 3) * 16);
+        const int row = 8 * quarter + 2 * j + (lane >> 4);
+        const uint4 w = lds128u(out + row * 256 + (piece ^ (row & 7)) * 16);
         if (row >= c.rows) continue;
         T* p = y + row * c.ldy + piece * 8;
         if (units >= 8) {
@@ -194,19 +208,20 @@ __device__ __forceinline__ void store_pieces(T* y, const Chunk& c, Frag& acc, in
                 if (i < units) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
         }
     }
-    __syncwarp();
+    bar_sync_128(4 + half);
 }
 
-template <bool MX, bool PAIR, int TN>
+template <bool MX, bool PAIR, int TN, bool SPLIT>
 __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
-    using S = Shape<MX, PAIR, TN>;
+    using S = Shape<MX, PAIR, TN, SPLIT>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    Control* ctl = reinterpret_cast<Control*>(smem + S::STAGES * S::STAGE + S::OUT_BYTES);
+    constexpr int OUT_AT = S::STAGES * S::STAGE;
+    Control* ctl = reinterpret_cast<Control*>(smem + OUT_AT + S::OUT_BYTES);
     volatile int* abort_flag = &ctl->wait.abort;
     pdl_trigger();
     const int warp = warp_index(), lane = threadIdx.x & 31;
-    const int rank = PAIR ? (int)cluster_rank() : 0;
+    const int rank = PAIR ? (int)cluster_rank() : 0, part = SPLIT ? (int)cluster_rank() : 0;
     constexpr int CTAS = PAIR ? 2 : 1;
 
     if (threadIdx.x == 0) {
@@ -257,32 +272,34 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
     }
     tc_fence_before_sync();
     __syncthreads();
-    if constexpr (PAIR) cluster_sync();
+    if constexpr (PAIR || SPLIT) cluster_sync();     // the others have started
     tc_fence_after_sync();
     const uint32_t tmem = ctl->tmem_base;
 
     const int unit_tiles = ceil_div(g.N, BM * CTAS), nks = ceil_div(g.K, BK);
-    const long long total = (long long)ctl->tiles[g.groups] * unit_tiles;
-    const int step = gridDim.x / CTAS;
+    const int total = ctl->tiles[g.groups] * unit_tiles;
+    // this CTA's (pair's) tiles; with SPLIT a cluster has one tile at most, and a CTA its share of the steps of K
+    const int workers = gridDim.x / (SPLIT ? g.split : CTAS), worker = blockIdx.x / (SPLIT ? g.split : CTAS);
+    const int k0 = SPLIT ? nks * part / g.split : 0, k1 = SPLIT ? nks * (part + 1) / g.split : nks;
 
     if (warp == TMA_WARP) {
         if (lane == 0) {
             int s = 0;
             uint32_t ph = 1;
             bool ok = true;
-            for (long long w = blockIdx.x / CTAS; w < total && ok; w += step) {
-                const Tile t = tile_at<TN>(ctl, g, (int)w, unit_tiles, BM * CTAS);
+            for (int w = worker; w < total && ok; w += workers) {
+                const Tile t = tile_at<TN>(ctl, g, w, unit_tiles, BM * CTAS);
                 const int cols = columns_of<PAIR>(t.n);
                 const int mine = PAIR ? cols / 2 : cols, boxes = ceil_div(mine, g.box);
                 const int unit = t.unit0 + rank * BM, row = t.row0 + rank * mine;
                 const int w_row = t.g * g.N + unit;
                 const int w_tile = (int)((long long)t.g * g.N / 128) + t.g + unit / 128;
                 const uint32_t bytes = S::A_BYTES + boxes * g.box * BK_BYTES + S::SFA_BYTES + S::SFB_BYTES;
-                for (int ks = 0; ks < nks; ++ks) {
+                for (int ks = k0; ks < k1; ++ks) {
                     ok = mbar_wait(smem_u32(&ctl->empty[s]), ph, abort_flag);
                     if (!ok) break;
-                    const uint32_t dst = smem_u32(smem) + s * S::STAGE, bar = smem_u32(&ctl->full[s]);
-                    const uint32_t bar0 = PAIR ? peer_addr(bar, 0) : bar;
+                    const uint32_t a = smem_u32(smem) + s * S::STAGE, b = a + S::A_BYTES, sf = b + S::B_BYTES;
+                    const uint32_t bar = smem_u32(&ctl->full[s]), bar0 = PAIR ? peer_addr(bar, 0) : bar;
                     if (rank == 0) mbar_arrive_expect_tx(bar, CTAS * bytes);
                     auto load = [&](uint32_t to, const CUtensorMap* map, int x, int y) {
                         if constexpr (PAIR) tma_load_2d_pair(to, map, x, y, bar0);
@@ -292,9 +309,8 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
                         if constexpr (PAIR) tma_load_3d_pair(to, map, 0, katom, tile, bar0);
                         else tma_load_3d(to, map, 0, katom, tile, bar);
                     };
-                    load(dst, &maps.w, ks * BK_BYTES, w_row);
-                    for (int b = 0; b < boxes; ++b) load(dst + S::A_BYTES + b * g.box * BK_BYTES, &maps.a, ks * BK_BYTES, row + b * g.box);
-                    const uint32_t sf = dst + S::A_BYTES + S::B_BYTES;
+                    load(a, &maps.w, ks * BK_BYTES, w_row);
+                    for (int i = 0; i < boxes; ++i) load(b + i * g.box * BK_BYTES, &maps.a, ks * BK_BYTES, row + i * g.box);
                     load_scales(sf, &maps.w_scales, ks * S::KATOMS, w_tile);
                     load_scales(sf + S::SFA_BYTES, &maps.a_scales, ks * S::KATOMS, t.a_tile);
                     if (++s == S::STAGES) { s = 0; ph ^= 1u; }
@@ -306,8 +322,8 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         int s = 0, buf = 0;
         uint32_t ph = 0, pfree = 1;       // a fresh barrier passes parity 1
         bool ok = rank == 0;
-        for (long long w = blockIdx.x / CTAS; w < total && ok; w += step) {
-            const Tile t = tile_at<TN>(ctl, g, (int)w, unit_tiles, BM * CTAS);
+        for (int w = worker; w < total && ok; w += workers) {
+            const Tile t = tile_at<TN>(ctl, g, w, unit_tiles, BM * CTAS);
             const int cols = columns_of<PAIR>(t.n);
             const uint32_t id0 = instr_desc_f4(BM * CTAS, cols, MX, 0), id2 = instr_desc_f4(BM * CTAS, cols, MX, MX ? 2 : 0);
             // the accumulator before this one is read as far as this one overlaps it, and all of the one before that
@@ -315,13 +331,13 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
             if (!ok) break;
             pfree ^= 1u;
             tc_fence_after_sync();
-            const uint32_t d = tmem + buf * S::ACC_STEP, sfa = tmem + SF_COL, sfb = sfa + 8;
-            for (int ks = 0; ks < nks; ++ks) {
+            const uint32_t d = tmem + buf * S::ACC_STEP, sfa = tmem + SF_COL, sfb = sfa + 8, sfo = t.sf_off;
+            for (int ks = k0; ks < k1; ++ks) {
                 ok = warp_wait(smem_u32(&ctl->full[s]), ph, abort_flag, lane);
                 if (!ok) break;
                 tc_fence_after_sync();
-                const uint32_t base = smem_u32(smem) + s * S::STAGE, sf = base + S::A_BYTES + S::B_BYTES;
-                const uint64_t da = smem_desc_sw128(base), db = smem_desc_sw128(base + S::A_BYTES);
+                const uint32_t a = smem_u32(smem) + s * S::STAGE, b = a + S::A_BYTES, sf = b + S::B_BYTES;
+                const uint64_t da = smem_desc_sw128(a), db = smem_desc_sw128(b);
                 const int left = g.K - ks * BK;
                 if (elect_one()) {
                     // Halves of 128 positions: their scales, then two MMAs of 64.  The copies and MMAs of one thread run in
@@ -334,15 +350,15 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
                             const int katom = h * (S::KATOMS / 2) + c;
                             tmem_copy_scales<PAIR>(sfa + 4 * c, sf + katom * 512);
 #pragma unroll
-                            for (int b = 0; b < S::ROW_TILES; ++b)
-                                tmem_copy_scales<PAIR>(sfb + 4 * S::ROW_TILES * c + 4 * b, sf + S::SFA_BYTES + (b * S::KATOMS + katom) * 512);
+                            for (int r = 0; r < S::ROW_TILES; ++r)
+                                tmem_copy_scales<PAIR>(sfb + 4 * S::ROW_TILES * c + 4 * r, sf + S::SFA_BYTES + (r * S::KATOMS + katom) * 512);
                         }
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
                             if (h * 128 + m * 64 >= left) break;
                             const int x = (h * 2 + m) * 2;       // 32 bytes, in units of 16
                             mma_f4<MX, PAIR>(d, da + x, db + x, MX && m ? id2 : id0, MX ? sfa : sfa + 4 * m,
-                                             MX ? sfb : sfb + 4 * S::ROW_TILES * m, (ks | h | m) != 0);
+                                             (MX ? sfb : sfb + 4 * S::ROW_TILES * m) + sfo, ks != k0 || h != 0 || m != 0);
                         }
                     }
                     if constexpr (PAIR) mma_commit_pair(smem_u32(&ctl->empty[s]));
@@ -357,26 +373,47 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
             buf ^= 1;
         }
         __syncwarp();
+    } else if constexpr (SPLIT) {
+        // this part's sums to shared memory, [row][unit]
+        const int half = warp >> 2, quarter = warp & 3;
+        if (worker < total) {
+            const Tile t = tile_at<TN>(ctl, g, worker, unit_tiles, BM);
+            if (warp_wait_relaxed(smem_u32(&ctl->acc_full), 0u, abort_flag, lane)) {
+                tc_fence_after_sync();
+                float* sums = reinterpret_cast<float*>(smem + OUT_AT) + quarter * 32 + lane;
+#pragma unroll 1
+                for (int at = half; at * 32 < t.n; at += 2) {
+                    uint32_t acc[32];
+                    tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + at * 32, acc);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (at * 32 + j < t.n) sums[(at * 32 + j) * BM] = __uint_as_float(acc[j]);
+                }
+            }
+        }
     } else {
         const int half = warp >> 2, quarter = warp & 3;
         const uint32_t free0 = PAIR ? peer_addr(smem_u32(&ctl->acc_free), 0) : smem_u32(&ctl->acc_free);
-        const uint32_t out = smem_u32(smem) + S::STAGES * S::STAGE + warp * OUT_CHUNK;
+        const uint32_t out = smem_u32(smem) + OUT_AT + half * 4 * OUT_CHUNK;
         uint32_t pfull = 0;
         int buf = 0;
-        for (long long w = blockIdx.x / CTAS; w < total; w += step) {
-            const Tile t = tile_at<TN>(ctl, g, (int)w, unit_tiles, BM * CTAS);
+        for (int w = worker; w < total; w += workers) {
+            const Tile t = tile_at<TN>(ctl, g, w, unit_tiles, BM * CTAS);
             const int u0 = t.unit0 + rank * BM + quarter * 32, chunks = ceil_div(t.n, 32);
-            // per-unit affine: of the lane's unit, or (16-bit results) of units lane / 4 + 8 i
+            // per-unit affine (the factor is a power of two: it may as well multiply the scale): of the lane's unit, or (16-bit results) of units lane / 4 + 8 i
             const bool pieces = g.pieces;
             const size_t p = (size_t)t.g * g.N + u0;
             float scale[4], shift[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int u = pieces ? (lane >> 2) + 8 * i : lane;
-                scale[i] = g.scale && u0 + u < g.N ? __ldg(g.scale + p + u) : 1.0f;
+                scale[i] = (g.scale && u0 + u < g.N ? __ldg(g.scale + p + u) : 1.0f) * g.factor;
                 shift[i] = g.shift && u0 + u < g.N ? __ldg(g.shift + p + u) : 0.0f;
             }
-            if (!warp_wait_relaxed(smem_u32(&ctl->acc_full), pfull, abort_flag, lane)) break;
+            // (the four warps of a half take the same decision: they meet at barriers below)
+            const bool ok = warp_wait_relaxed(smem_u32(&ctl->acc_full), pfull, abort_flag, lane);
+            if (!(half ? epi_all_b(ok) : epi_all(ok))) break;
             pfull ^= 1u;
             tc_fence_after_sync();
             const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * S::ACC_STEP);
@@ -394,19 +431,20 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
             // the columns that the next tile's accumulator overlaps come first: the highest of the first one, the lowest
             // of the second
             const int mine = (chunks - half + 1) >> 1;
-            Chunk c{g.factor, g.ldy, g.N - u0, 0};
+            Chunk c{g.ldy, g.N - u0, 0};
             auto chunk_at = [&](int i) { return half + 2 * (buf == 0 ? mine - 1 - i : i); };
             auto by_pieces = [&](auto* y, auto act) {
                 Frag acc;
                 acc.load(taddr + chunk_at(0) * 32);
+                Chunk whole{g.ldy, g.N - t.unit0 - rank * BM, 0};
 #pragma unroll 1
                 for (int i = 0; i < mine; ++i) {
                     const int at = chunk_at(i);
-                    c.rows = min(32, t.n - at * 32);
+                    whole.rows = min(32, t.n - at * 32);
                     tmem_ld_wait();
                     read();
-                    store_pieces<decltype(act)::value>(y + (t.row0 + at * 32) * g.ldy + u0, c, acc, lane, out, scale, shift, i + 1 < mine,
-                                                       taddr + chunk_at(i + 1) * 32);
+                    store_pieces<decltype(act)::value>(y + (t.row0 + at * 32) * g.ldy + t.unit0 + rank * BM, whole, acc, half, quarter, lane, out,
+                                                       scale, shift, i + 1 < mine, taddr + chunk_at(i + 1) * 32);
                 }
             };
             auto by_units = [&](auto* y, auto act) {
@@ -433,7 +471,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
                         read();
 #pragma unroll
                         for (int j = 0; j < 32; ++j) {
-                            const float v = fmaf(scale[0], __uint_as_float(acc[j]) * g.factor, shift[0]);
+                            const float v = fmaf(scale[0], __uint_as_float(acc[j]), shift[0]);
                             const uint32_t b = __ballot_sync(0xFFFFFFFFu, lane < c.units && sign_is_pos(v, g.sign_mode));
                             if (lane == j) word = b;
                         }
@@ -452,6 +490,62 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         }
     }
 
+    if constexpr (SPLIT) {
+        // every CTA adds up its share of the rows from all parts, a warp a row and a lane four units, its own part first
+        __syncwarp();
+        cluster_sync();
+        if (warp < EPI_WARPS && worker < total) {
+            const Tile t = tile_at<TN>(ctl, g, worker, unit_tiles, BM);
+            const int per = ceil_div(t.n, g.split), end = min((part + 1) * per, t.n), unit = t.unit0 + lane * 4, units = g.N - unit;
+            const size_t p = (size_t)t.g * g.N + unit;
+            float scale[4], shift[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                scale[i] = (g.scale && i < units ? __ldg(g.scale + p + i) : 1.0f) * g.factor;
+                shift[i] = g.shift && i < units ? __ldg(g.shift + p + i) : 0.0f;
+            }
+            for (int r = part * per + warp; r < end; r += EPI_WARPS) {
+                const uint32_t at = smem_u32(smem) + OUT_AT + (r * BM + lane * 4) * 4;
+                float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+                for (int i = 0; i < g.split; ++i) {
+                    const float4 x = ld_cluster4(peer_addr(at, (part + i) & (g.split - 1)));
+                    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+                }
+                uint32_t bits = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = fmaf(scale[i], v[i], shift[i]);
+                    bits |= (i < units && sign_is_pos(v[i], g.sign_mode) ? 1u : 0u) << ((lane & 7) * 4 + i);
+                    v[i] = g.act == BNN_ACT_HARDTANH ? activate<BNN_ACT_HARDTANH>(v[i]) : g.act == BNN_ACT_SIGMOID ? activate<BNN_ACT_SIGMOID>(v[i]) : v[i];
+                }
+                const long long row = t.row0 + r;
+                if (g.out_bits) {
+#pragma unroll
+                    for (int d = 1; d < 8; d <<= 1) bits |= __shfl_xor_sync(0xFFFFFFFFu, bits, d);
+                    if (!(lane & 7) && units > 0) g.out_bits[row * g.ldob + (unit >> 5)] = bits;
+                } else {
+                    const long long to = row * g.ldy + unit;
+                    if (g.dtype != BNN_DTYPE_F32 && g.pieces && units >= 4) {
+                        const uint2 w = g.dtype == BNN_DTYPE_F16 ? make_uint2(pack2(v[0], v[1], __half()), pack2(v[2], v[3], __half()))
+                                                                 : make_uint2(pack2(v[0], v[1], __nv_bfloat16()), pack2(v[2], v[3], __nv_bfloat16()));
+                        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.Y) + to) = w;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (i >= units) break;
+                            if (g.dtype == BNN_DTYPE_F32) put(static_cast<float*>(g.Y) + to + i, v[i]);
+                            else if (g.dtype == BNN_DTYPE_F16) put(static_cast<__half*>(g.Y) + to + i, v[i]);
+                            else put(static_cast<__nv_bfloat16*>(g.Y) + to + i, v[i]);
+                        }
+                    }
+                }
+            }
+        }
+        __syncwarp();
+        cluster_sync();          // nobody reads this CTA's sums any more
+    }
+
     // every thread arrives here, also after a wait that ran out
     __syncwarp();
     tc_fence_before_sync();
@@ -465,16 +559,16 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
     if (threadIdx.x == 0 && ctl->wait.abort) atomicExch(g.status.word, 1);
 }
 
-template <bool MX, int TN>
+template <bool MX, int TN, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1) f4_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args g) {
-    body<MX, false, TN>(maps, g);
+    body<MX, false, TN, SPLIT>(maps, g);
 }
 
 // The same on pairs of CTAs: 256 units x up to 256 rows, half of the rows in the shared memory of each.
 template <bool MX>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 f4_gemm_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args g) {
-    body<MX, true, 256>(maps, g);
+    body<MX, true, PAIR_ROWS, false>(maps, g);
 }
 
 template <typename S>
@@ -486,22 +580,41 @@ bool encode_maps(Maps* m, const F4GemmArgs& a, int kt, int box) {
            encode_scale_map(&m->a_scales, a.a_scales, f4::row_tiles(a.M, a.groups), kt, S::ROW_TILES, S::KATOMS);
 }
 
-template <bool MX, bool PAIR, int TN>
+// An upper bound on the tiles of a form: the groups' rows are only known on the device.
+long long tiles_of(const F4GemmArgs& a, int rows, int units) {
+    return (a.M / rows + (a.offsets ? (long long)(a.M < a.groups ? a.M : a.groups) : 1)) * ceil_div(a.N, units);
+}
+
+template <bool MX, bool PAIR, int TN, bool SPLIT>
 int launch_form(const F4GemmArgs& a, Args g, int box, int sms, cudaStream_t st) {
-    using S = Shape<MX, PAIR, TN>;
+    using S = Shape<MX, PAIR, TN, SPLIT>;
     constexpr int CTAS = PAIR ? 2 : 1;
     Maps maps;
     g.box = box;
     void (*kern)(Maps, Args);
     if constexpr (PAIR) kern = f4_gemm_pair_kernel<MX>;
-    else kern = f4_gemm_kernel<MX, TN>;
+    else kern = f4_gemm_kernel<MX, TN, SPLIT>;
     if (!ensure_dynamic_smem(reinterpret_cast<const void*>(kern), S::SMEM) || !encode_maps<S>(&maps, a, g.kt, box)) return BNN_ERR_CUDA;
-    // an upper bound on the tiles: the groups' rows are only known on the device
-    const long long row_tiles = a.M / TN + (a.offsets ? (a.M < a.groups ? a.M : a.groups) : 1);
-    const long long tiles = row_tiles * ceil_div(a.N, BM * CTAS);
-    const int grid = CTAS * (int)(tiles < sms / CTAS ? tiles : sms / CTAS);
-    if (launch_pdl(kern, dim3(grid), dim3(THREADS), S::SMEM, st, maps, g) != cudaSuccess) return BNN_ERR_CUDA;
+    const long long tiles = tiles_of(a, TN, BM * CTAS);
+    if constexpr (SPLIT) {
+        if (launch_pdl_cluster(kern, dim3((unsigned)(tiles * g.split)), dim3(THREADS), g.split, S::SMEM, st, maps, g) != cudaSuccess) return BNN_ERR_CUDA;
+    } else {
+        const int grid = CTAS * (int)(tiles < sms / CTAS ? tiles : sms / CTAS);
+        if (launch_pdl(kern, dim3(grid), dim3(THREADS), S::SMEM, st, maps, g) != cudaSuccess) return BNN_ERR_CUDA;
+    }
     return launch_status();
+}
+
+// Up to 32 rows: clusters of 2 or 4 CTAs share a tile's K where the tiles alone leave SMs idle.  (Quantisation and product, one row,
+// us without and with: K = N = 2048 6.9 and 6.3, 4096 10.0 and 7.7, 8192 15.6 and 12.2, K = 8192 N = 2048 15.2 and 8.8.  Clusters of 8
+// wait for so many free SMs of a GPC that they lose: 10.4 at 2048.  So does adding up 128 rows and more: 256 rows of 2048 8.2 and 11.5.)
+template <bool MX>
+int launch_few_rows(const F4GemmArgs& a, Args g, int sms, cudaStream_t st) {
+    const long long tiles = tiles_of(a, 32, BM);
+    const int box = a.M <= 16 ? 16 : 32;
+    g.split = 1;
+    while (g.split < MAX_SPLIT && tiles * g.split * 2 <= sms && g.split * 2 <= ceil_div(a.K, BK)) g.split *= 2;
+    return g.split > 1 ? launch_form<MX, false, 32, true>(a, g, box, sms, st) : launch_form<MX, false, 32, false>(a, g, box, sms, st);
 }
 
 // Which form.  Up to 32 rows: tiles of 32 (a group's second tile of 32 would start inside a tile of scales, so that these are 32
@@ -511,15 +624,15 @@ int launch_form(const F4GemmArgs& a, Args g, int box, int sms, cudaStream_t st) 
 // bytes, and narrow tiles have more of them on their way: 2048 rows by 32 groups 21.2 and 19.3, 4096 rows 27.1 and 27.4.
 template <bool MX>
 int launch_format(const F4GemmArgs& a, const Args& g, int sms, cudaStream_t st) {
-    if (a.M <= 32) return launch_form<MX, false, 32>(a, g, 32, sms, st);
+    if (a.M <= 32) return launch_few_rows<MX>(a, g, sms, st);
     const int rows = a.offsets ? ceil_div(a.M, a.groups) : a.M;      // of a group, on average
     auto turns = [&](int tile, int ctas) {
         // (half a tile for the rest of each group)
         const long long row_tiles = a.offsets ? a.M / tile + (a.groups + 1) / 2 : ceil_div(a.M, tile);
         return (row_tiles * ceil_div(a.N, BM * ctas) + sms / ctas - 1) / (sms / ctas);
     };
-    if (rows >= 128 && sms >= 2 && 5 * turns(256, 2) < 4 * turns(128, 1)) return launch_form<MX, true, 256>(a, g, 128, sms, st);
-    return launch_form<MX, false, 128>(a, g, rows <= 32 ? 32 : rows <= 64 ? 64 : 128, sms, st);
+    if (rows >= 128 && sms >= 2 && 5 * turns(256, 2) < 4 * turns(128, 1)) return launch_form<MX, true, PAIR_ROWS, false>(a, g, PAIR_ROWS / 2, sms, st);
+    return launch_form<MX, false, 128, false>(a, g, rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128, sms, st);
 }
 
 }  // namespace

@@ -136,6 +136,8 @@ __device__ __forceinline__ bool epi_all_b(bool pred) {
         : "=r"(r) : "r"((uint32_t)pred) : "memory");
     return r != 0;
 }
+// Barrier `id` of 128 threads.
+__device__ __forceinline__ void bar_sync_128(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ void epi_bar_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 // 16-byte store to a shared-space address (keeps the compiler from using generic stores).
@@ -300,6 +302,12 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
 // Arrive on a barrier of either CTA (address from peer_addr).
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// Load from a shared-cluster address (peer_addr).
+__device__ __forceinline__ float4 ld_cluster4(uint32_t cluster_addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
+    return v;
 }
 // Allocation by one warp of EACH CTA of the pair, and release.
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t slot_smem, uint32_t ncols) {

@@ -50,7 +50,8 @@ def dtype_of(torch, name):
     (33, 140, 288), (64, 100, 513), (100, 257, 1000), (128, 128, 384), (129, 384, 224), (200, 77, 640), (255, 200, 31), (256, 128, 512),
     (257, 300, 100), (300, 129, 1100), (511, 640, 300), (513, 260, 2048), (1100, 900, 700),
     # enough tiles for pairs of CTAs
-    (1100, 2304, 300), (2050, 1300, 513), (1537, 2561, 64), (2300, 1290, 1100), (1290, 2056, 32)])
+    (1100, 2304, 300), (2050, 1300, 513), (1537, 2561, 64), (2300, 1290, 1100), (1290, 2056, 32),
+    (1100, 2304, 2600), (1290, 2304, 2048), (2300, 1290, 4200)])
 def test_product(env, fmt, M, N, K):
     torch, B = env
     rng = np.random.default_rng(M * 31 + N * 7 + K)
