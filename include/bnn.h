@@ -579,6 +579,14 @@ BNN_API int bnn_route_experts(const void* logits, int dtype, int T, int E, int l
 BNN_API int bnn_combine_experts(const void* Z, int z_dtype, int rows, int ldz, const int32_t* slot, const float* weight,
                         int T, int k, int N, void* Y, int y_dtype, int ldy, void* stream);
 
+/* The calls above with their arguments as consecutive 64-bit words, in the order of their declarations (pointers as
+ * addresses, ints sign-extended): for bindings that convert argument by argument, which takes a microsecond of a call's seven.
+ * words : HOST, n of them.  Returns what the call returns; BNN_ERR_UNSUPPORTED for an unknown call, BNN_ERR_SHAPE where n is not
+ * its number of arguments or a word does not fit its argument, BNN_ERR_NULL without words. */
+typedef enum { BNN_CALL_F4_QUANTIZE = 0, BNN_CALL_F4_DEQUANTIZE = 1, BNN_CALL_F4_GEMM = 2, BNN_CALL_F4_GEMM_GROUPED = 3,
+               BNN_CALL_ROUTE_EXPERTS = 4, BNN_CALL_COMBINE_EXPERTS = 5 } bnn_call;
+BNN_API int bnn_call_words(int call, const int64_t* words, int n);
+
 /* Smallest legal packed pitch (in words) for rows of K bits: ceil(K/32) rounded up to 4. */
 BNN_API int bnn_packed_pitch(int K);
 

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -511,12 +512,36 @@ def _dtype(t):
     return d
 
 
+_get_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None
+
+
 def _here(tensors):
     """All tensors given lie on the device that the call runs on."""
-    dev = torch._C._cuda_getDevice()
+    dev = _get_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError("expected a tensor on the current CUDA device %d, got one on %s" % (dev, t.device))
+
+
+class _Call:
+    """An entry point whose arguments are handed over as one block of 64-bit words (bnn_call_words): ctypes takes 60 ns to
+    convert an argument, and these have up to twenty."""
+
+    def __init__(self, name, number, arguments):
+        self.name, self.number, self.n, self.pack, self.f = name, number, arguments, struct.Struct("%dq" % arguments).pack, None
+
+    def __call__(self, *args):
+        f = self.f
+        if f is None:
+            f = self.f = lib()["bnn_call_words"]      # a prototype of its own: two ints and a block of bytes
+        rc = f(self.number, self.pack(*args), self.n)
+        if rc:
+            raise BnnError(rc, self.name)
+
+
+_f4_quantize, _f4_dequantize = _Call("bnn_f4_quantize", 0, 16), _Call("bnn_f4_dequantize", 1, 14)
+_f4_gemm, _f4_gemm_grouped = _Call("bnn_f4_gemm", 2, 18), _Call("bnn_f4_gemm_grouped", 3, 20)
+_route_experts, _combine_experts = _Call("bnn_route_experts", 4, 15), _Call("bnn_combine_experts", 5, 13)
 
 
 def _refuse(what):
@@ -548,7 +573,7 @@ def _scales(t):
 def _groups(offsets):
     """(address, number of groups)"""
     if offsets is None:
-        return None, 1
+        return 0, 1
     n = offsets.numel()
     return _flat(offsets, torch.int32, n, "offsets"), n - 1
 
@@ -565,42 +590,42 @@ def bnn_f4_scale_bytes(fmt, rows, K, groups=1) -> int:
 def bnn_f4_quantize(X, codes, scales, fmt=F4_E8M0_32, source=None, offsets=None, exponent=0):
     """Rows of X (gathered by ``source``) -> ``codes`` (uint8 [rows][pitch]) and ``scales`` (uint8, bnn_f4_scale_bytes)."""
     _here((X, codes, scales, source, offsets))
-    rows = codes.shape[0]
-    off, groups = _groups(offsets)
-    sc, sb = _scales(scales)
-    src = None if source is None else _flat(source, torch.int32, rows, "source")
-    _check(lib().bnn_f4_quantize(X.data_ptr(), _dtype(X), X.shape[0], X.shape[1], _ld(X), src, off, groups, rows, fmt, exponent,
-                                 *_codes(codes), sc, sb, _stream()), "bnn_f4_quantize")
+    rows, (src_rows, k) = codes.shape[0], X.shape
+    src = 0 if source is None else _flat(source, torch.int32, rows, "source")
+    _f4_quantize(X.data_ptr(), _dtype(X), src_rows, k, _ld(X), src, *_groups(offsets), rows, fmt, exponent, *_codes(codes),
+                 *_scales(scales), _stream())
     return codes, scales
 
 
 def bnn_f4_dequantize(codes, scales, Y, fmt=F4_E8M0_32, offsets=None, exponent=0):
     """The values of a quantised matrix, in Y's type."""
     _here((codes, scales, Y, offsets))
-    if codes.shape[0] != Y.shape[0]:
+    rows, k = Y.shape
+    if codes.shape[0] != rows:
         _refuse("codes and Y have different numbers of rows")
-    off, groups = _groups(offsets)
-    sc, sb = _scales(scales)
-    _check(lib().bnn_f4_dequantize(*_codes(codes), sc, sb, off, groups, Y.shape[0], Y.shape[1], fmt, exponent,
-                                   Y.data_ptr(), _dtype(Y), _ld(Y), _stream()), "bnn_f4_dequantize")
+    _f4_dequantize(*_codes(codes), *_scales(scales), *_groups(offsets), rows, k, fmt, exponent, Y.data_ptr(), _dtype(Y), _ld(Y), _stream())
     return Y
 
 
-def _f4_output(rows, n, y, act, sign_mode, scale, shift, out_bits, per):
-    """(Y, dtype, ldy, epilogue)"""
-    epi = None
-    if act != ACT_NONE or scale is not None or shift is not None or out_bits is not None:
-        for t in (scale, shift):
-            if t is not None:
-                _flat(t, torch.float32, per, "scale, shift")
-        if out_bits is not None and out_bits.shape[0] != rows:
-            _refuse("out_bits has another number of rows")
-        epi = C.byref(_epilogue(act, sign_mode, scale, shift, out_bits=out_bits))
+def _f4_epilogue(rows, n, act, sign_mode, scale, shift, out_bits):
+    """The epilogue of a product; None where there is nothing to it."""
+    if act == ACT_NONE and scale is None and shift is None and out_bits is None:
+        return None
+    for t in (scale, shift):
+        if t is not None:
+            _flat(t, torch.float32, n, "scale, shift")
+    if out_bits is not None and out_bits.shape[0] != rows:
+        _refuse("out_bits has another number of rows")
+    return _epilogue(act, sign_mode, scale, shift, out_bits=out_bits)
+
+
+def _f4_result(y, rows, n):
+    """(address, type, pitch)"""
     if y is None:
-        return None, 0, 0, epi
+        return 0, 0, 0
     if y.shape != (rows, n):
         _refuse("Y: expected [%d, %d]" % (rows, n))
-    return y.data_ptr(), _dtype(y), _ld(y), epi
+    return y.data_ptr(), _dtype(y), _ld(y)
 
 
 def bnn_f4_gemm(A, a_scales, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0, act=ACT_NONE, scale=None, shift=None,
@@ -608,10 +633,9 @@ def bnn_f4_gemm(A, a_scales, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0,
     """Y = act(fma(scale, 2^exponent * A W^T, shift)) of two quantised matrices (codes uint8 [rows][pitch], scales)."""
     _here((A, a_scales, W, w_scales, Y, scale, shift, out_bits))
     m, n = A.shape[0], W.shape[0]
-    (sa, ba), (sw, bw) = _scales(a_scales), _scales(w_scales)
-    y, dt, ldy, epi = _f4_output(m, n, Y, act, sign_mode, scale, shift, out_bits, n)
-    _check(lib().bnn_f4_gemm(*_codes(A), sa, ba, *_codes(W), sw, bw, m, n, K, fmt, exponent,
-                             y, dt, ldy, epi, _stream()), "bnn_f4_gemm")
+    e = _f4_epilogue(m, n, act, sign_mode, scale, shift, out_bits)
+    _f4_gemm(*_codes(A), *_scales(a_scales), *_codes(W), *_scales(w_scales), m, n, K, fmt, exponent, *_f4_result(Y, m, n),
+             0 if e is None else C.addressof(e), _stream())
     return Y if out_bits is None else out_bits
 
 
@@ -623,11 +647,10 @@ def bnn_f4_gemm_grouped(A, a_scales, offsets, W, w_scales, K, Y=None, fmt=F4_E8M
     shape, stride = W.shape, W.stride()
     if len(shape) != 3 or shape[0] != groups or (groups > 1 and stride[0] != shape[1] * stride[1]):
         _refuse("W: expected [%d, N, pitch], the groups one behind the other" % groups)
-    m, n = A.shape[0], W.shape[1]
-    (sa, ba), (sw, bw) = _scales(a_scales), _scales(w_scales)
-    y, dt, ldy, epi = _f4_output(m, n, Y, act, sign_mode, scale, shift, out_bits, groups * n)
-    _check(lib().bnn_f4_gemm_grouped(*_codes(A), sa, ba, off, groups, *_codes(W, 3), sw, bw,
-                                     m, n, K, fmt, exponent, y, dt, ldy, epi, _stream()), "bnn_f4_gemm_grouped")
+    m, n = A.shape[0], shape[1]
+    e = _f4_epilogue(m, groups * n, act, sign_mode, scale, shift, out_bits)
+    _f4_gemm_grouped(*_codes(A), *_scales(a_scales), off, groups, *_codes(W, 3), *_scales(w_scales), m, n, K, fmt, exponent,
+                     *_f4_result(Y, m, n), 0 if e is None else C.addressof(e), _stream())
     return Y if out_bits is None else out_bits
 
 
@@ -638,14 +661,13 @@ def bnn_route_workspace_bytes(T, E) -> int:
 def bnn_route_experts(logits, index, weight, offsets, slot, source, workspace, mode=ROUTE_SOFTMAX):
     """The k best experts of each token, their weights, and the tokens sorted by expert (k = index.shape[1])."""
     _here((logits, index, weight, offsets, slot, source, workspace))
-    (t, e), k = logits.shape, index.shape[1]
-    if index.shape[0] != t:
+    (t, e), (rows, k) = logits.shape, index.shape
+    if rows != t:
         _refuse("index has another number of tokens")
     i32, n = torch.int32, t * k
-    _check(lib().bnn_route_experts(logits.data_ptr(), _dtype(logits), t, e, _ld(logits), k, mode, _flat(index, i32, n, "index"),
-                                   _flat(weight, torch.float32, n, "weight"), _flat(offsets, i32, e + 1, "offsets"),
-                                   _flat(slot, i32, n, "slot"), _flat(source, i32, n, "source"), *_scales(workspace),
-                                   _stream()), "bnn_route_experts")
+    _route_experts(logits.data_ptr(), _dtype(logits), t, e, _ld(logits), k, mode, _flat(index, i32, n, "index"),
+                   _flat(weight, torch.float32, n, "weight"), _flat(offsets, i32, e + 1, "offsets"), _flat(slot, i32, n, "slot"),
+                   _flat(source, i32, n, "source"), *_scales(workspace), _stream())
     return index, weight, offsets, slot, source
 
 
@@ -655,7 +677,6 @@ def bnn_combine_experts(Z, slot, weight, Y):
     (t, k), (rows, n) = slot.shape, Z.shape
     if Y.shape != (t, n):
         _refuse("Y: expected [%d, %d]" % (t, n))
-    _check(lib().bnn_combine_experts(Z.data_ptr(), _dtype(Z), rows, _ld(Z), _flat(slot, torch.int32, t * k, "slot"),
-                                     _flat(weight, torch.float32, t * k, "weight"), t, k, n, Y.data_ptr(), _dtype(Y), _ld(Y),
-                                     _stream()), "bnn_combine_experts")
+    _combine_experts(Z.data_ptr(), _dtype(Z), rows, _ld(Z), _flat(slot, torch.int32, t * k, "slot"),
+                     _flat(weight, torch.float32, t * k, "weight"), t, k, n, Y.data_ptr(), _dtype(Y), _ld(Y), _stream())
     return Y

@@ -1,5 +1,9 @@
 // extern "C" boundary of the operators on 4-bit floating point and on experts: argument validation.  No allocation, no sync.
+#include <limits.h>
 #include <math.h>
+
+#include <type_traits>
+#include <utility>
 
 #include "f4.cuh"
 
@@ -78,9 +82,40 @@ int gemm_checked(const void* a, int lda, const void* a_scales, size_t a_scale_by
     return launch_f4_gemm(g, static_cast<cudaStream_t>(stream));
 }
 
+// A call whose arguments come as words.
+template <typename T>
+bool fits(int64_t w) { return !std::is_same<T, int>::value || (w >= INT_MIN && w <= INT_MAX); }
+template <typename T>
+T from_word(int64_t w) {
+    if constexpr (std::is_pointer<T>::value) return reinterpret_cast<T>(static_cast<uintptr_t>(w));
+    else return static_cast<T>(w);
+}
+template <typename... Args, size_t... I>
+int call_words(int (*f)(Args...), const int64_t* w, std::index_sequence<I...>) {
+    if (!(fits<Args>(w[I]) && ...)) return BNN_ERR_SHAPE;
+    return f(from_word<Args>(w[I])...);
+}
+template <typename... Args>
+int call_words(int (*f)(Args...), const int64_t* w, int n) {
+    return n == (int)sizeof...(Args) ? call_words(f, w, std::index_sequence_for<Args...>()) : BNN_ERR_SHAPE;
+}
+
 }  // namespace
 
 extern "C" {
+
+int bnn_call_words(int call, const int64_t* words, int n) {
+    if (!words) return BNN_ERR_NULL;
+    switch (call) {
+        case BNN_CALL_F4_QUANTIZE: return call_words(bnn_f4_quantize, words, n);
+        case BNN_CALL_F4_DEQUANTIZE: return call_words(bnn_f4_dequantize, words, n);
+        case BNN_CALL_F4_GEMM: return call_words(bnn_f4_gemm, words, n);
+        case BNN_CALL_F4_GEMM_GROUPED: return call_words(bnn_f4_gemm_grouped, words, n);
+        case BNN_CALL_ROUTE_EXPERTS: return call_words(bnn_route_experts, words, n);
+        case BNN_CALL_COMBINE_EXPERTS: return call_words(bnn_combine_experts, words, n);
+        default: return BNN_ERR_UNSUPPORTED;
+    }
+}
 
 int bnn_f4_pitch(int K) { return K < 1 || K > f4::kMaxK ? 0 : f4::code_bytes(K); }
 

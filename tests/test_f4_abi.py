@@ -36,21 +36,27 @@ def refused(B, name, good, status, **bad):
     assert B.raw_call(name, *{**good, **bad}.values()) == status, (name, bad)
 
 
-@pytest.mark.parametrize("bad,status", [
+QUANTIZE_BAD = [
     (dict(X=None), NULL), (dict(codes=None), NULL), (dict(scales=None), NULL), (dict(fmt=2), UNSUPPORTED), (dict(fmt=-1), UNSUPPORTED),
     (dict(dtype=3), UNSUPPORTED), (dict(rows=0), SHAPE), (dict(K=0), SHAPE), (dict(K=BIG, ldx=BIG), SHAPE), (dict(ldx=99), SHAPE),
     (dict(src_rows=0), SHAPE), (dict(src_rows=299), SHAPE), (dict(groups=0), SHAPE), (dict(groups=2), SHAPE), (dict(offsets=FAKE, groups=1025), SHAPE),
     (dict(exponent=65), SHAPE), (dict(exponent=-65), SHAPE), (dict(ldc=48), SHAPE), (dict(ldc=72), ALIGN), (dict(codes=FAKE + 8), ALIGN),
     (dict(scales=FAKE + 4), ALIGN), (dict(X=FAKE + 2), ALIGN), (dict(source=FAKE + 1), ALIGN), (dict(offsets=FAKE + 2, groups=1), ALIGN),
-    (dict(scale_bytes=3 * 512 - 1), WORKSPACE), (dict(fmt=1), WORKSPACE), (dict(offsets=FAKE, groups=2), WORKSPACE)])
+    (dict(scale_bytes=3 * 512 - 1), WORKSPACE), (dict(fmt=1), WORKSPACE), (dict(offsets=FAKE, groups=2), WORKSPACE)]
+
+
+@pytest.mark.parametrize("bad,status", QUANTIZE_BAD)
 def test_quantize(B, bad, status):
     refused(B, "bnn_f4_quantize", QUANTIZE, status, **bad)
 
 
-@pytest.mark.parametrize("bad,status", [
+DEQUANTIZE_BAD = [
     (dict(Y=None), NULL), (dict(codes=None), NULL), (dict(scales=None), NULL), (dict(fmt=7), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED),
     (dict(rows=0), SHAPE), (dict(K=0), SHAPE), (dict(ldy=99), SHAPE), (dict(ldc=48), SHAPE), (dict(ldc=65), ALIGN), (dict(Y=FAKE + 2), ALIGN),
-    (dict(exponent=100), SHAPE), (dict(groups=3), SHAPE), (dict(scale_bytes=0), WORKSPACE)])
+    (dict(exponent=100), SHAPE), (dict(groups=3), SHAPE), (dict(scale_bytes=0), WORKSPACE)]
+
+
+@pytest.mark.parametrize("bad,status", DEQUANTIZE_BAD)
 def test_dequantize(B, bad, status):
     refused(B, "bnn_f4_dequantize", DEQUANTIZE, status, **bad)
 
@@ -68,8 +74,11 @@ def test_product(B, bad, status):
     refused(B, "bnn_f4_gemm", GEMM, status, **bad)
 
 
-@pytest.mark.parametrize("bad,status", PRODUCT + [(dict(offsets=None), NULL), (dict(offsets=FAKE + 1), ALIGN), (dict(groups=0), SHAPE),
-                                                  (dict(groups=1025), SHAPE), (dict(groups=1024, N=1 << 21), SHAPE)])
+GROUPED_BAD = PRODUCT + [(dict(offsets=None), NULL), (dict(offsets=FAKE + 1), ALIGN), (dict(groups=0), SHAPE),
+                                                  (dict(groups=1025), SHAPE), (dict(groups=1024, N=1 << 21), SHAPE)]
+
+
+@pytest.mark.parametrize("bad,status", GROUPED_BAD)
 def test_grouped_product(B, bad, status):
     refused(B, "bnn_f4_gemm_grouped", GROUPED, status, **bad)
 
@@ -88,19 +97,25 @@ def test_epilogues(B, fields, bad, status):
     refused(B, "bnn_f4_gemm_grouped", GROUPED, status, epi=C.byref(e), **bad)
 
 
-@pytest.mark.parametrize("bad,status", [
+ROUTE_BAD = [
     *[({n: None}, NULL) for n in ("logits", "index", "weight", "offsets", "slot", "source")], (dict(workspace=None), WORKSPACE),
     (dict(bytes=3), WORKSPACE), (dict(T=1000), WORKSPACE), (dict(dtype=3), UNSUPPORTED), (dict(mode=2), UNSUPPORTED), (dict(T=0), SHAPE),
     (dict(E=0), SHAPE), (dict(E=1025, ld=1025), SHAPE), (dict(ld=63), SHAPE), (dict(k=0), SHAPE), (dict(k=33), SHAPE), (dict(k=5, E=4), SHAPE),
-    (dict(T=1 << 28, k=8), SHAPE), (dict(logits=FAKE + 2), ALIGN), (dict(weight=FAKE + 2), ALIGN), (dict(slot=FAKE + 1), ALIGN)])
+    (dict(T=1 << 28, k=8), SHAPE), (dict(logits=FAKE + 2), ALIGN), (dict(weight=FAKE + 2), ALIGN), (dict(slot=FAKE + 1), ALIGN)]
+
+
+@pytest.mark.parametrize("bad,status", ROUTE_BAD)
 def test_router(B, bad, status):
     refused(B, "bnn_route_experts", ROUTE, status, **bad)
 
 
-@pytest.mark.parametrize("bad,status", [
+COMBINE_BAD = [
     *[({n: None}, NULL) for n in ("Z", "slot", "weight", "Y")], (dict(z_dtype=3), UNSUPPORTED), (dict(y_dtype=-1), UNSUPPORTED), (dict(rows=0), SHAPE),
     (dict(T=0), SHAPE), (dict(k=0), SHAPE), (dict(k=33), SHAPE), (dict(N=0), SHAPE), (dict(ldz=63), SHAPE), (dict(ldy=63), SHAPE),
-    (dict(Z=FAKE + 2), ALIGN), (dict(y_dtype=2, Y=FAKE + 1), ALIGN), (dict(slot=FAKE + 2), ALIGN), (dict(weight=FAKE + 2), ALIGN)])
+    (dict(Z=FAKE + 2), ALIGN), (dict(y_dtype=2, Y=FAKE + 1), ALIGN), (dict(slot=FAKE + 2), ALIGN), (dict(weight=FAKE + 2), ALIGN)]
+
+
+@pytest.mark.parametrize("bad,status", COMBINE_BAD)
 def test_weighted_sum(B, bad, status):
     refused(B, "bnn_combine_experts", COMBINE, status, **bad)
 
@@ -140,3 +155,31 @@ def test_the_reference_rounds_to_the_nearest():
                 s = F(2.0 ** (float(byte[r, k // n]) - 127)) if fmt == ref.MX else F(float(ref.E4M3[byte[r, k // n]]))
                 best = min(abs(min(abs(F(float(x[r, k]))), 6 * s) - F(float(g)) * s) for g in ref.E2M1)
                 assert abs(min(abs(F(float(x[r, k]))), 6 * s) - abs(F(float(v[r, k])))) == best
+
+
+@pytest.mark.parametrize("number,name,good,bads", [
+    (0, "bnn_f4_quantize", QUANTIZE, QUANTIZE_BAD), (1, "bnn_f4_dequantize", DEQUANTIZE, DEQUANTIZE_BAD), (2, "bnn_f4_gemm", GEMM, PRODUCT),
+    (3, "bnn_f4_gemm_grouped", GROUPED, GROUPED_BAD), (4, "bnn_route_experts", ROUTE, ROUTE_BAD), (5, "bnn_combine_experts", COMBINE, COMBINE_BAD)])
+def test_arguments_as_words(B, number, name, good, bads):
+    """bnn_call_words: the refusals of the calls, and its own."""
+    import struct
+
+    def words(call, values):
+        values = [v or 0 for v in values]
+        return B.lib()["bnn_call_words"](call, struct.pack("%dq" % len(values), *values), len(values))
+    for bad, status in bads:
+        assert words(number, {**good, **bad}.values()) == status, bad
+    values = list(good.values())
+    assert words(number, values[:-1]) == words(number, values + [0]) == SHAPE
+    ints = [i for i, t in enumerate(getattr(B.lib(), name).argtypes) if t is C.c_int]
+    assert len(ints) >= 6
+    for at in ints:
+        for v in (1 << 31, -(1 << 31) - 1, (1 << 32) + values[at]):      # would be another int if it were cut
+            assert words(number, values[:at] + [v] + values[at + 1:]) == SHAPE, (at, v)
+    assert words(6, values) == words(-1, values) == UNSUPPORTED
+    assert B.lib()["bnn_call_words"](number, None, len(values)) == NULL
+
+
+def test_the_bindings_hand_over_as_many_words_as_the_calls_have_arguments(B):
+    for c in (B._f4_quantize, B._f4_dequantize, B._f4_gemm, B._f4_gemm_grouped, B._route_experts, B._combine_experts):
+        assert c.n == len(getattr(B.lib(), c.name).argtypes), c.name
