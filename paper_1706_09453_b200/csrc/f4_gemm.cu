@@ -59,7 +59,7 @@ struct Args {
     float factor;
     const float* scale;
     const float* shift;
-    int act, sign_mode, box, split;
+    int act, sign_mode, box, split, tile_rows;
     void* Y;
     int dtype, pieces;
     long long ldy;
@@ -93,14 +93,13 @@ __device__ __forceinline__ int group_of(const Control* ctl, int groups, int j) {
     }
     return lo;
 }
-template <int TN>
-__device__ __forceinline__ Tile make_tile(const Control* ctl, int group, int row_tile, int unit0) {
+__device__ __forceinline__ Tile make_tile(const Control* ctl, int tile_rows, int group, int row_tile, int unit0) {
     Tile t;
     t.g = group;
     t.unit0 = unit0;
-    const int off = row_tile * TN, begin = ctl->first[group];
+    const int off = row_tile * tile_rows, begin = ctl->first[group];
     t.row0 = begin + off;
-    t.n = min(TN, ctl->first[group + 1] - t.row0);
+    t.n = min(tile_rows, ctl->first[group + 1] - t.row0);
     t.a_tile = begin / 128 + group + off / 128;
     t.sf_off = (off & 127) >> 5;
     return t;
@@ -109,11 +108,10 @@ __device__ __forceinline__ Tile make_tile(const Control* ctl, int group, int row
 // Tile number w: panels of PANEL unit tiles, in which the units run fastest, so that the tiles that run at the same time
 // are about as many unit tiles as row tiles and share both operands' reads.  (Consecutive tiles for a CTA, whose weights then stay
 // in shared memory, are slower: 8192 x 4096 x 8192 113 us instead of 108, 32 groups 89 instead of 83.)
-template <int TN>
 __device__ __forceinline__ Tile tile_at(const Control* ctl, const Args& g, int w, int unit_tiles, int unit_step) {
     const int rows = ctl->tiles[g.groups], panel = w / (rows * PANEL), in = w - panel * rows * PANEL;
     const int wide = min(PANEL, unit_tiles - panel * PANEL), j = in / wide, group = group_of(ctl, g.groups, j);
-    return make_tile<TN>(ctl, group, j - ctl->tiles[group], (panel * PANEL + in - j * wide) * unit_step);
+    return make_tile(ctl, g.tile_rows, group, j - ctl->tiles[group], (panel * PANEL + in - j * wide) * unit_step);
 }
 
 template <bool PAIR>
@@ -252,7 +250,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
             int before = 0;
             for (int i0 = 0; i0 < g.groups; i0 += 32) {
                 const int i = i0 + lane;
-                const int mine = i < g.groups ? (max(ctl->first[i + 1] - ctl->first[i], 0) + TN - 1) / TN : 0;
+                const int mine = i < g.groups ? (max(ctl->first[i + 1] - ctl->first[i], 0) + g.tile_rows - 1) / g.tile_rows : 0;
                 int sum = mine;
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
@@ -268,7 +266,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         ctl->first[0] = 0;
         ctl->first[1] = g.M;
         ctl->tiles[0] = 0;
-        ctl->tiles[1] = ceil_div(g.M, TN);
+        ctl->tiles[1] = ceil_div(g.M, g.tile_rows);
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -288,7 +286,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
             uint32_t ph = 1;
             bool ok = true;
             for (int w = worker; w < total && ok; w += workers) {
-                const Tile t = tile_at<TN>(ctl, g, w, unit_tiles, BM * CTAS);
+                const Tile t = tile_at(ctl, g, w, unit_tiles, BM * CTAS);
                 const int cols = columns_of<PAIR>(t.n);
                 const int mine = PAIR ? cols / 2 : cols, boxes = ceil_div(mine, g.box);
                 const int unit = t.unit0 + rank * BM, row = t.row0 + rank * mine;
@@ -323,7 +321,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         uint32_t ph = 0, pfree = 1;       // a fresh barrier passes parity 1
         bool ok = rank == 0;
         for (int w = worker; w < total && ok; w += workers) {
-            const Tile t = tile_at<TN>(ctl, g, w, unit_tiles, BM * CTAS);
+            const Tile t = tile_at(ctl, g, w, unit_tiles, BM * CTAS);
             const int cols = columns_of<PAIR>(t.n);
             const uint32_t id0 = instr_desc_f4(BM * CTAS, cols, MX, 0), id2 = instr_desc_f4(BM * CTAS, cols, MX, MX ? 2 : 0);
             // the accumulator before this one is read as far as this one overlaps it, and all of the one before that
@@ -377,7 +375,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         // this part's sums to shared memory, [row][unit]
         const int half = warp >> 2, quarter = warp & 3;
         if (worker < total) {
-            const Tile t = tile_at<TN>(ctl, g, worker, unit_tiles, BM);
+            const Tile t = tile_at(ctl, g, worker, unit_tiles, BM);
             if (warp_wait_relaxed(smem_u32(&ctl->acc_full), 0u, abort_flag, lane)) {
                 tc_fence_after_sync();
                 float* sums = reinterpret_cast<float*>(smem + OUT_AT) + quarter * 32 + lane;
@@ -399,7 +397,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         uint32_t pfull = 0;
         int buf = 0;
         for (int w = worker; w < total; w += workers) {
-            const Tile t = tile_at<TN>(ctl, g, w, unit_tiles, BM * CTAS);
+            const Tile t = tile_at(ctl, g, w, unit_tiles, BM * CTAS);
             const int u0 = t.unit0 + rank * BM + quarter * 32, chunks = ceil_div(t.n, 32);
             // per-unit affine (the factor is a power of two: it may as well multiply the scale): of the lane's unit, or (16-bit results) of units lane / 4 + 8 i
             const bool pieces = g.pieces;
@@ -495,7 +493,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         __syncwarp();
         cluster_sync();
         if (warp < EPI_WARPS && worker < total) {
-            const Tile t = tile_at<TN>(ctl, g, worker, unit_tiles, BM);
+            const Tile t = tile_at(ctl, g, worker, unit_tiles, BM);
             const int per = ceil_div(t.n, g.split), end = min((part + 1) * per, t.n), unit = t.unit0 + lane * 4, units = g.N - unit;
             const size_t p = (size_t)t.g * g.N + unit;
             float scale[4], shift[4];
@@ -586,16 +584,17 @@ long long tiles_of(const F4GemmArgs& a, int rows, int units) {
 }
 
 template <bool MX, bool PAIR, int TN, bool SPLIT>
-int launch_form(const F4GemmArgs& a, Args g, int box, int sms, cudaStream_t st) {
+int launch_form(const F4GemmArgs& a, Args g, int tile_rows, int box, int sms, cudaStream_t st) {
     using S = Shape<MX, PAIR, TN, SPLIT>;
     constexpr int CTAS = PAIR ? 2 : 1;
     Maps maps;
     g.box = box;
+    g.tile_rows = tile_rows;
     void (*kern)(Maps, Args);
     if constexpr (PAIR) kern = f4_gemm_pair_kernel<MX>;
     else kern = f4_gemm_kernel<MX, TN, SPLIT>;
     if (!ensure_dynamic_smem(reinterpret_cast<const void*>(kern), S::SMEM) || !encode_maps<S>(&maps, a, g.kt, box)) return BNN_ERR_CUDA;
-    const long long tiles = tiles_of(a, TN, BM * CTAS);
+    const long long tiles = tiles_of(a, tile_rows, BM * CTAS);
     if constexpr (SPLIT) {
         if (launch_pdl_cluster(kern, dim3((unsigned)(tiles * g.split)), dim3(THREADS), g.split, S::SMEM, st, maps, g) != cudaSuccess) return BNN_ERR_CUDA;
     } else {
@@ -614,25 +613,35 @@ int launch_few_rows(const F4GemmArgs& a, Args g, int sms, cudaStream_t st) {
     const int box = a.M <= 16 ? 16 : 32;
     g.split = 1;
     while (g.split < MAX_SPLIT && tiles * g.split * 2 <= sms && g.split * 2 <= ceil_div(a.K, BK)) g.split *= 2;
-    return g.split > 1 ? launch_form<MX, false, 32, true>(a, g, box, sms, st) : launch_form<MX, false, 32, false>(a, g, box, sms, st);
+    return g.split > 1 ? launch_form<MX, false, 32, true>(a, g, 32, box, sms, st) : launch_form<MX, false, 32, false>(a, g, 32, box, sms, st);
 }
 
 // Which form.  Up to 32 rows: tiles of 32 (a group's second tile of 32 would start inside a tile of scales, so that these are 32
-// rows in all).  Else single CTAs (128 x 128) or pairs (256 x 256), by the turns that the SMs take and what a turn
-// costs: measured, a pair's is 1.1 (many turns) to 1.25 (one turn) of a single CTA's.  2048 rows, K = N = 2048: pairs 8.7 us, single 10.9;
-// 1024 rows: 9.0 and 7.0; 8192 x 4096 x 8192: 108 and 199.  Groups of less than 128 rows on average are bound by their weights'
-// bytes, and narrow tiles have more of them on their way: 2048 rows by 32 groups 21.2 and 19.3, 4096 rows 27.1 and 27.4.
+// rows in all).  Else single CTAs (128 units x 128 rows), pairs of 256 units x 256 rows, or, without groups, of 192 rows (every second tile then
+// starts in the middle of a tile of scales), by the clocks that the SMs are estimated to take: the turns, what each takes as measured on
+// many turns (the epilogue's time where K is short), and the last one's epilogue.  Measured, us single / 192 / 256: 1024 rows, K = N =
+// 2048 6.8 / 8.0 / 8.1; 731 rows, N = 3307 11.1 / 9.0 / 9.4; 2048 rows 11.0 / 11.3 / 8.6; 4096 x 4096 x 4096 47.3 / 36.6 / 31.5; 4096 x 512 x
+// 4096 16.4 / 15.3 / 14.6; 16384 rows by 32 groups of 2048 x 4096 118 / 90 / 80.  (Pairs of 128 rows win nowhere.)
+// Groups of less than 128 rows on average are bound by their weights' bytes, and narrow tiles have more of them on their way: 2048
+// rows by 32 groups 19.3 and 21.2.
 template <bool MX>
 int launch_format(const F4GemmArgs& a, const Args& g, int sms, cudaStream_t st) {
     if (a.M <= 32) return launch_few_rows<MX>(a, g, sms, st);
     const int rows = a.offsets ? ceil_div(a.M, a.groups) : a.M;      // of a group, on average
-    auto turns = [&](int tile, int ctas) {
+    const long long steps = ceil_div(a.K, BK);
+    auto clocks = [&](int tile, int ctas, long long shortest, long long step, long long more, long long last) {
         // (half a tile for the rest of each group)
         const long long row_tiles = a.offsets ? a.M / tile + (a.groups + 1) / 2 : ceil_div(a.M, tile);
-        return (row_tiles * ceil_div(a.N, BM * ctas) + sms / ctas - 1) / (sms / ctas);
+        const long long turns = (row_tiles * ceil_div(a.N, BM * ctas) + sms / ctas - 1) / (sms / ctas), turn = steps * step + more;
+        return turns * (turn > shortest ? turn : shortest) + last;
     };
-    if (rows >= 128 && sms >= 2 && 5 * turns(256, 2) < 4 * turns(128, 1)) return launch_form<MX, true, PAIR_ROWS, false>(a, g, PAIR_ROWS / 2, sms, st);
-    return launch_form<MX, false, 128, false>(a, g, rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128, sms, st);
+    if (rows >= 128 && sms >= 2) {
+        const long long single = clocks(128, 1, 3500, 753, 1450, 1900), high = clocks(256, 2, 5200, 743, 2350, 3800);
+        const long long low = a.offsets ? high : clocks(192, 2, 3900, 700, 2200, 3000);
+        if (low < high && low < single) return launch_form<MX, true, PAIR_ROWS, false>(a, g, 192, 96, sms, st);
+        if (high < single) return launch_form<MX, true, PAIR_ROWS, false>(a, g, 256, 128, sms, st);
+    }
+    return launch_form<MX, false, 128, false>(a, g, 128, rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128, sms, st);
 }
 
 }  // namespace

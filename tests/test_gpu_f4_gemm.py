@@ -51,7 +51,9 @@ def dtype_of(torch, name):
     (257, 300, 100), (300, 129, 1100), (511, 640, 300), (513, 260, 2048), (1100, 900, 700),
     # enough tiles for pairs of CTAs
     (1100, 2304, 300), (2050, 1300, 513), (1537, 2561, 64), (2300, 1290, 1100), (1290, 2056, 32),
-    (1100, 2304, 2600), (1290, 2304, 2048), (2300, 1290, 4200)])
+    (1100, 2304, 2600), (1290, 2304, 2048), (2300, 1290, 4200),
+    # pairs whose tiles have 192 rows
+    (731, 3307, 300), (576, 4700, 2050), (700, 3300, 1000)])
 def test_product(env, fmt, M, N, K):
     torch, B = env
     rng = np.random.default_rng(M * 31 + N * 7 + K)
