@@ -71,7 +71,7 @@ struct Args {
 template <int A> struct Act { static constexpr int value = A; };
 
 struct Control {
-    uint64_t full[MAX_STAGES], empty[MAX_STAGES], acc_full, acc_free;
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], acc_full, acc_free, drained;
     WaitState wait;
     uint32_t tmem_base;
     int first[f4::kMaxGroups + 1];      // first row of each group, held inside 0 .. M
@@ -228,6 +228,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
             mbar_init(smem_u32(&ctl->empty[s]), 1);     // a commit
         }
         mbar_init(smem_u32(&ctl->acc_full), 1);
+        mbar_init(smem_u32(&ctl->drained), 1);
         mbar_init(smem_u32(&ctl->acc_free), CTAS * EPI_WARPS);
         wait_state_init(&ctl->wait, g.status);
         mbar_init_fence();
@@ -280,6 +281,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
     const int workers = gridDim.x / (SPLIT ? g.split : CTAS), worker = blockIdx.x / (SPLIT ? g.split : CTAS);
     const int k0 = SPLIT ? nks * part / g.split : 0, k1 = SPLIT ? nks * (part + 1) / g.split : nks;
 
+    int issued = 0;                      // steps that the copying thread has asked for
     if (warp == TMA_WARP) {
         if (lane == 0) {
             int s = 0;
@@ -299,6 +301,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
                     const uint32_t a = smem_u32(smem) + s * S::STAGE, b = a + S::A_BYTES, sf = b + S::B_BYTES;
                     const uint32_t bar = smem_u32(&ctl->full[s]), bar0 = PAIR ? peer_addr(bar, 0) : bar;
                     if (rank == 0) mbar_arrive_expect_tx(bar, CTAS * bytes);
+                    ++issued;
                     auto load = [&](uint32_t to, const CUtensorMap* map, int x, int y) {
                         if constexpr (PAIR) tma_load_2d_pair(to, map, x, y, bar0);
                         else tma_load_2d(to, map, x, y, bar);
@@ -548,6 +551,22 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
     __syncwarp();
     tc_fence_before_sync();
     __syncthreads();
+    if (*abort_flag) {
+        // what is still on its way ends first: the MMAs and the copies (of a pair: those of both CTAs, counted on rank 0)
+        if (warp == MMA_WARP) {
+            if (rank == 0 && elect_one()) {
+                if constexpr (PAIR) mma_commit_pair(smem_u32(&ctl->drained));
+                else mma_commit(smem_u32(&ctl->drained));
+            }
+            __syncwarp();
+            mbar_wait_out(smem_u32(&ctl->drained), 0u, g.status.limit);
+        } else if (warp == TMA_WARP && lane == 0 && rank == 0) {
+            for (int i = max(0, issued - S::STAGES); i < issued; ++i)
+                mbar_wait_out(smem_u32(&ctl->full[i % S::STAGES]), (uint32_t)(i / S::STAGES) & 1u, g.status.limit);
+        }
+        __syncwarp();
+        __syncthreads();
+    }
     if constexpr (PAIR) cluster_sync();
     if (warp == MMA_WARP) {
         tc_fence_after_sync();

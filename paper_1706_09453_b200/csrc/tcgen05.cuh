@@ -76,6 +76,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     return true;
 }
 
+// The same on the way out, after another wait has run out: bounded by the clock alone.
+__device__ __forceinline__ void mbar_wait_out(uint32_t bar, uint32_t parity, long long limit) {
+    const long long t0 = clock64();
+#pragma unroll 1
+    while (!mbar_try_wait(bar, parity))
+        if (clock64() - t0 > limit) return;
+}
+
 // Wait of a role that has slack (an epilogue warp waiting for a whole tile of MMAs, the thread
 // that refills a staging ring): the polls carry a suspend-time hint, so the waiter sleeps in
 // hardware instead of competing with the producers for the shared-memory pipe.  It may wake a

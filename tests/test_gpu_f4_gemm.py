@@ -243,3 +243,77 @@ def test_rows_further_apart_than_32_bits_hold(env, name):
     got = y.double().cpu().numpy()
     assert (np.abs(got - want) <= (0 if name == "f32" else 2.0 ** -8) * np.abs(want)).all()
     assert torch.equal(z, y)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 700, 2048), (20, 300, 1100), (90, 900, 700), (1100, 2304, 600)])
+def test_captured_products_on_two_streams(env, M, N, K):
+    """Two products of each form captured into graphs and replayed side by side, on new values each time."""
+    torch, B = env
+    rng = np.random.default_rng(M)
+    runs = []
+    for fmt in (ref.MX, ref.NV):
+        a, w = ref.random_stored(rng, M, K, fmt, 0), ref.random_stored(rng, N, K, fmt, 0)
+        (ad, asc), (wd, wsc) = stored(torch, *a), stored(torch, *w)
+        y, g = torch.empty((M, N), device=DEV), torch.cuda.CUDAGraph()
+        B.bnn_f4_gemm(ad, asc, wd, wsc, K, y, fmt)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            for _ in range(3):
+                B.bnn_f4_gemm(ad, asc, wd, wsc, K, y, fmt)
+        runs.append((fmt, ad, asc, w, y, g, torch.cuda.Stream(), (wd, wsc)))     # (a graph keeps no tensor alive)
+    for turn in range(3):
+        news = []
+        for fmt, ad, asc, w, y, g, st, _ in runs:
+            a = ref.random_stored(rng, M, K, fmt, 0)
+            ad.copy_(torch.as_tensor(ref.pack(a[0]), device=DEV))
+            asc.copy_(torch.as_tensor(ref.store_scales(a[1], None, 1, 0xFF), device=DEV))
+            news.append(a)
+        torch.cuda.synchronize()
+        for fmt, ad, asc, w, y, g, st, _ in runs:
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        for a, (fmt, ad, asc, w, y, g, st, _) in zip(news, runs):
+            # scales of 1: the sums are multiples of 1/4 that fp32 holds
+            np.testing.assert_array_equal(y.double().cpu().numpy(), product(ref.values(*a, fmt, K), ref.values(*w, fmt, K))[0])
+    assert B.bnn_device_status() == 0
+
+
+def test_the_binding_refuses_what_does_not_fit(env):
+    torch, B = env
+    u8 = dict(dtype=torch.uint8, device=DEV)
+    M, N, K = 5, 40, 96
+    a, w, y = torch.zeros((M, 48), **u8), torch.zeros((N, 48), **u8), torch.zeros((M, N), device=DEV)
+    sa, sw = torch.zeros((512,), **u8), torch.zeros((512,), **u8)
+    B.bnn_f4_gemm(a, sa, w, sw, K, y)
+    for bad in (dict(A=a.cpu()), dict(w_scales=sw.cpu()), dict(Y=y[:4]), dict(Y=y.t().contiguous()), dict(Y=y[:, :39]), dict(A=a.float()),
+                dict(W=w.t()), dict(a_scales=sa.int()), dict(shift=torch.zeros(N + 1, device=DEV)), dict(scale=torch.zeros(N, device=DEV).half())):
+        with pytest.raises((ValueError, TypeError)):
+            B.bnn_f4_gemm(**{**dict(A=a, a_scales=sa, W=w, w_scales=sw, K=K, Y=y), **bad})
+    for bad, status in ((dict(K=97), 2), (dict(a_scales=sa[:256]), 5), (dict(exponent=65), 2), (dict(fmt=7), 4), (dict(Y=None), 1)):
+        with pytest.raises(B.BnnError) as e:
+            B.bnn_f4_gemm(**{**dict(A=a, a_scales=sa, W=w, w_scales=sw, K=K, Y=y), **bad})
+        assert e.value.status == status and "bnn_f4_gemm" in str(e.value)
+    off = torch.zeros((3,), dtype=torch.int32, device=DEV)
+    for bad in (w, w.view(4, 10, 48), torch.zeros((2, 2 * 20, 48), **u8)[:, :20]):
+        with pytest.raises(ValueError):
+            B.bnn_f4_gemm_grouped(a, torch.zeros((1024,), **u8), off, bad, torch.zeros((2048,), **u8), K, y[:, :20])
+    with pytest.raises(ValueError):
+        B.bnn_f4_quantize(torch.zeros((9, K), device=DEV), a, sa, source=torch.zeros((4,), dtype=torch.int32, device=DEV))
+    with pytest.raises(TypeError):
+        B.bnn_f4_quantize(torch.zeros((M, K), device=DEV, dtype=torch.float64), a, sa)
+    with pytest.raises(ValueError):
+        B.bnn_f4_dequantize(a, sa, torch.zeros((4, K), device=DEV))
+    i32 = dict(dtype=torch.int32, device=DEV)
+    route = dict(logits=torch.zeros((6, 8), device=DEV), index=torch.zeros((6, 2), **i32), weight=torch.zeros((6, 2), device=DEV), offsets=torch.zeros((9,), **i32),
+                 slot=torch.zeros((6, 2), **i32), source=torch.zeros((12,), **i32), workspace=torch.zeros((64,), **u8))
+    B.bnn_route_experts(**route)
+    for bad in (dict(index=torch.zeros((5, 2), **i32)), dict(offsets=torch.zeros((8,), **i32)), dict(source=torch.zeros((11,), **i32)), dict(weight=route["weight"].half()),
+                dict(slot=torch.zeros((6, 3), **i32)), dict(logits=route["logits"].t())):
+        with pytest.raises(ValueError):
+            B.bnn_route_experts(**{**route, **bad})
+    z, yy = torch.zeros((12, 40), device=DEV), torch.zeros((6, 40), device=DEV)
+    for bad in ((z, route["slot"], route["weight"], yy[:5]), (z, route["slot"], route["weight"][:, :1], yy), (z[:, :39], route["slot"], route["weight"], yy)):
+        with pytest.raises(ValueError):
+            B.bnn_combine_experts(*bad)
+    assert B.bnn_device_status() == 0
