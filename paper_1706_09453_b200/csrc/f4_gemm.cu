@@ -9,6 +9,12 @@
 // with TMA, one warp moves the scales to tensor memory (tcgen05.cp) and issues the MMAs, eight warps empty the accumulator.
 // Two accumulators alternate.  Tiles of 256 columns leave 512 - 2 * 256 = 0 columns for the scales, so these accumulators
 // overlap by 32 columns, which the epilogue reads first: the next tile starts as soon as they are read.
+//
+// Bound by the bytes that an SM takes in from L2: 42.5 a clock, which plain loads reach as well.  A step of a pair (256 units x 256
+// rows x 256 of K) is 36 KB, 843 clocks, for 512 of MMA; without any MMA 8192 x 4096 x 4096 takes 49.7 us instead of 52.9.  On top come
+// the stores (without them 97 us instead of 106 at 8192 x 4096 x 8192, 5.2 PFLOP/s) and, where K is short, the epilogue, 5200 clocks a
+// tile.  Each TMA instruction costs as well: two copies of 64 rows and scale tiles one by one instead of one copy per operand were 118
+// us instead of 109.  e4m3 scales, of which there are twice as many, take 112.  Scale copies to tensor memory cost nothing measurable.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -243,25 +249,35 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         }
     }
     pdl_wait();
-    // Groups: offsets that make no sense are held inside the matrix, and a group never ends before it starts.
+    // Groups.  Offsets that make no sense are held inside the matrix and made to ascend, so that no row is in two groups.
     if (g.offsets) {
         for (int i = threadIdx.x; i <= g.groups; i += THREADS) ctl->first[i] = min(max(__ldg(g.offsets + i), 0), g.M);
         __syncthreads();
         if (warp == 0) {
-            int before = 0;
-            for (int i0 = 0; i0 < g.groups; i0 += 32) {
-                const int i = i0 + lane;
-                const int mine = i < g.groups ? (max(ctl->first[i + 1] - ctl->first[i], 0) + g.tile_rows - 1) / g.tile_rows : 0;
-                int sum = mine;
+            int most = 0, before = 0;
+            for (int i0 = 0; i0 <= g.groups; i0 += 32) {
+                const int i = i0 + lane, lowest = most;
+                int first = i <= g.groups ? ctl->first[i] : 0;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int o = __shfl_up_sync(0xFFFFFFFFu, first, d);
+                    if (lane >= d) first = max(first, o);
+                }
+                first = max(first, lowest);
+                if (i <= g.groups) ctl->first[i] = first;
+                most = __shfl_sync(0xFFFFFFFFu, first, 31);
+                // tiles of group i - 1
+                int prev = __shfl_up_sync(0xFFFFFFFFu, first, 1);
+                if (lane == 0) prev = lowest;
+                int sum = i > 0 && i <= g.groups ? (first - prev + g.tile_rows - 1) / g.tile_rows : 0;
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
                     const int o = __shfl_up_sync(0xFFFFFFFFu, sum, d);
                     if (lane >= d) sum += o;
                 }
-                if (i < g.groups) ctl->tiles[i] = before + sum - mine;
+                if (i <= g.groups) ctl->tiles[i] = before + sum;
                 before += __shfl_sync(0xFFFFFFFFu, sum, 31);
             }
-            if (lane == 0) ctl->tiles[g.groups] = before;
         }
     } else if (threadIdx.x == 0) {
         ctl->first[0] = 0;
@@ -402,7 +418,8 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         for (int w = worker; w < total; w += workers) {
             const Tile t = tile_at(ctl, g, w, unit_tiles, BM * CTAS);
             const int u0 = t.unit0 + rank * BM + quarter * 32, chunks = ceil_div(t.n, 32);
-            // per-unit affine (the factor is a power of two: it may as well multiply the scale): of the lane's unit, or (16-bit results) of units lane / 4 + 8 i
+            // per-unit affine (the factor is a power of two: it may as well multiply the scale): of the lane's unit, or (16-bit
+            // results) of units lane / 4 + 8 i
             const bool pieces = g.pieces;
             const size_t p = (size_t)t.g * g.N + u0;
             float scale[4], shift[4];
@@ -672,7 +689,8 @@ int launch_f4_gemm(const F4GemmArgs& a, cudaStream_t st) {
     g.kt = f4::scale_tiles(a.format, a.K);
     g.factor = a.factor; g.scale = a.scale; g.shift = a.shift; g.act = a.act; g.sign_mode = a.sign_mode;
     g.Y = a.Y; g.dtype = a.dtype; g.ldy = a.ldy;
-    g.pieces = a.Y && a.dtype != BNN_DTYPE_F32 && aligned16(a.Y) && a.ldy % 8 == 0; g.out_bits = a.out_bits; g.ldob = a.ldob;
+    g.pieces = a.Y && a.dtype != BNN_DTYPE_F32 && aligned16(a.Y) && a.ldy % 8 == 0;
+    g.out_bits = a.out_bits; g.ldob = a.ldob;
     g.status = tc_status();
     if (sms < 1 || !g.status.word) return BNN_ERR_CUDA;
     return a.format == BNN_F4_E8M0_32 ? launch_format<true>(a, g, sms, st) : launch_format<false>(a, g, sms, st);
