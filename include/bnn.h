@@ -538,13 +538,13 @@ BNN_API int bnn_f4_dequantize(const void* codes, int ldc, const void* scales, si
                       void* Y, int dtype, int ldy, void* stream);
 
 /* Product of two quantised matrices of one format, Eq. 1 with 4-bit weights and inputs:
- *   Y[m][n] = act(fma(scale[n], 2^exponent * sum_k a[m][k] w[n][k], shift[n]))
- * with fp32 sums.  A : [M] rows, W : [N] rows in the stored form above.  epi (may be NULL): scale, shift, and act
+ *   Y[m][n] = act(fma(2^exponent * scale[n], sum_k a[m][k] w[n][k], shift[n]))
+ * with fp32 sums, whose order depends on the sizes.  A : [M] rows, W : [N] rows in the stored form above.  epi (may be NULL): scale, shift, and act
  * BNN_ACT_NONE / HARDTANH / SIGMOID with Y [M][ldy] of `dtype`, or BNN_ACT_SIGN_PACK with Y NULL and out_bits (the input of a
  * binary layer).  Any M from one row on.
  * bnn_f4_gemm_grouped: group g's rows of A by W's rows g * N .. g * N + N - 1; W is [groups * N] rows whose scales are stored with
  * offsets[g] = g * N; scale and shift are [groups][N].
- * Errors: as bnn_f4_quantize; BNN_ERR_UNSUPPORTED also for an act that is not named above. */
+ * The results may not overlap the operands.  Errors: as bnn_f4_quantize; BNN_ERR_UNSUPPORTED also for an act that is not named above. */
 BNN_API int bnn_f4_gemm(const void* A, int lda, const void* a_scales, size_t a_scale_bytes,
                 const void* W, int ldw, const void* w_scales, size_t w_scale_bytes,
                 int M, int N, int K, int format, int exponent, void* Y, int dtype, int ldy,

@@ -630,7 +630,7 @@ def _f4_result(y, rows, n):
 
 def bnn_f4_gemm(A, a_scales, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0, act=ACT_NONE, scale=None, shift=None,
                 out_bits=None, sign_mode=SIGN_ZERO_POS):
-    """Y = act(fma(scale, 2^exponent * A W^T, shift)) of two quantised matrices (codes uint8 [rows][pitch], scales)."""
+    """Y = act(fma(2^exponent * scale, A W^T, shift)) of two quantised matrices (codes uint8 [rows][pitch], scales)."""
     _here((A, a_scales, W, w_scales, Y, scale, shift, out_bits))
     m, n = A.shape[0], W.shape[0]
     e = _f4_epilogue(m, n, act, sign_mode, scale, shift, out_bits)

@@ -5,7 +5,11 @@
 // token, its logits in registers as ordered integers; a pick is a warp maximum.  Within a block's tokens an expert has a
 // bit mask of the tokens that chose it, so that a rank is a popcount and no order of atomics can change a result.  Up to
 // kOneBlock tokens one block does it all; beyond, a first kernel chooses and counts by block, and a second one adds the
-// counts of the blocks before (behind a kernel that sums them, where there are many) and places.
+// counts of the blocks before (behind a kernel that sums them, where there are many) and places.  16384 tokens, 256 experts, eight
+// each, fp32: 22 us, 14 of them the choice (650 instructions of a warp per token; the logits' 17 MB are 2.6 us); 8 tokens, 64
+// experts: 3.4 us.
+//
+// Weighted sum: bound by memory, 8192 tokens with four rows of 4096 bf16 each 53.5 us (6.3 TB/s).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -1,5 +1,5 @@
 // Product of two quantised matrices, dense or by groups of rows (experts), on the block-scaled 4-bit tensor-core path:
-//   Y[m][n] = act(scale[n] * 2^e * sum_k a[m][k] w[n][k] + shift[n]),  a and w: e2m1 codes times their blocks' scales.
+//   Y[m][n] = act(2^e * scale[n] * sum_k a[m][k] w[n][k] + shift[n]),  a and w: e2m1 codes times their blocks' scales.
 //
 // The units (rows of W) are the MMA's M side and the activations' rows its N side: an N can be any multiple of 16, so a tile's
 // width follows the rows that a group has, down to a single token, while 128 units always fill the M side.  The accumulator then
@@ -418,8 +418,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
         for (int w = worker; w < total; w += workers) {
             const Tile t = tile_at(ctl, g, w, unit_tiles, BM * CTAS);
             const int u0 = t.unit0 + rank * BM + quarter * 32, chunks = ceil_div(t.n, 32);
-            // per-unit affine (the factor is a power of two: it may as well multiply the scale): of the lane's unit, or (16-bit
-            // results) of units lane / 4 + 8 i
+            // per-unit affine: of the lane's unit, or (16-bit results) of units lane / 4 + 8 i
             const bool pieces = g.pieces;
             const size_t p = (size_t)t.g * g.N + u0;
             float scale[4], shift[4];

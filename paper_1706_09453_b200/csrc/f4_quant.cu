@@ -7,8 +7,9 @@
 // a border between two codes only if the exact one does (a border times s has seven bits; the next fp32 number is
 // further off than half a step of the quotient).  Blocks with a NaN or an infinity get the scale NaN.
 //
-// Bound by memory: 8 elements a lane, 256 a warp and turn; the block's maximum is an integer maximum of magnitudes over two or
-// four lanes (NaNs are the largest).  A lane writes 4 bytes of codes, the first lane of a block the scale's byte.
+// Bound by memory where rows are read once: 16384 x 4096 bf16 take 25 us (172 MB, 6.9 TB/s), back 27 us (6.3 TB/s).  Gathered rows come mostly
+// from L2 and are bound by instructions (16384 from 4096 rows 24 us).  The block's
+// maximum is an integer maximum of magnitudes over its lanes (NaNs are the largest), two 16-bit ones at a time.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

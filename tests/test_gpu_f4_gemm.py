@@ -210,6 +210,48 @@ def test_groups(env, fmt, kind):
     assert B.bnn_device_status() == 0
 
 
+@pytest.mark.parametrize("fmt", [ref.MX, ref.NV])
+@pytest.mark.parametrize("rows", [12, 500, 3000])
+def test_groups_to_bits_and_other_pitches(env, fmt, rows):
+    """A binary layer behind each expert's layer: few rows, single CTAs and pairs; weights whose rows are further apart."""
+    torch, B = env
+    rng = np.random.default_rng(rows)
+    G, N, K = 4, 1290, 530
+    off = np.concatenate([[0], np.sort(rng.integers(0, rows, G - 1)), [rows]])
+    a, w = ref.random_stored(rng, rows, K, fmt), ref.random_stored(rng, G * N, K, fmt)
+    (ad, asc), (wd, wsc) = stored(torch, *a, offsets=off, groups=G), stored(torch, *w, offsets=np.arange(G + 1) * N, groups=G, pad=2)
+    scale, shift = rng.normal(0, 1, (G, N)).astype(np.float32), rng.normal(0, 20, (G, N)).astype(np.float32)
+    dev = lambda x: torch.as_tensor(x, device=DEV)
+    bits = torch.full((rows, B.packed_pitch(N)), -1, dtype=torch.int32, device=DEV)
+    B.bnn_f4_gemm_grouped(ad, asc, dev(off.astype(np.int32)), wd.view(G, N, -1), wsc, K, None, fmt, act=B.ACT_SIGN_PACK, scale=dev(scale), shift=dev(shift), out_bits=bits)
+    nw = (N + 31) // 32
+    got = (bits.cpu().numpy().view(np.uint32)[:, :nw, None] >> np.arange(32, dtype=np.uint32) & 1).reshape(rows, -1).astype(bool)
+    av, wv = ref.values(*a, fmt, K), ref.values(*w, fmt, K).reshape(G, N, K)
+    for g in range(G):
+        lo, hi = off[g], off[g + 1]
+        total, mag = product(av[lo:hi], wv[g])
+        pre = total * scale[g] + shift[g]
+        sure = np.abs(pre) > K * 2.0 ** -23 * mag * np.abs(scale[g]) + 2.0 ** -23 * np.abs(pre)
+        assert (got[lo:hi, :N] == (pre > 0))[sure].all()
+    assert not got[:, N:].any() and B.bnn_device_status() == 0
+
+
+def test_a_thousand_groups_on_pairs(env):
+    torch, B = env
+    rng = np.random.default_rng(6)
+    G, N, K = 1024, 600, 64
+    off = np.concatenate([[0], np.cumsum(rng.integers(0, 300, G))])
+    M = int(off[-1])
+    a, w = ref.random_stored(rng, M, K, ref.MX, 0), ref.random_stored(rng, G * N, K, ref.MX, 0)
+    (ad, asc), (wd, wsc) = stored(torch, *a, offsets=off, groups=G), stored(torch, *w, offsets=np.arange(G + 1) * N, groups=G)
+    y = torch.empty((M, N), device=DEV)
+    B.bnn_f4_gemm_grouped(ad, asc, torch.as_tensor(off.astype(np.int32), device=DEV), wd.view(G, N, -1), wsc, K, y, ref.MX)
+    got, av, wv = y.cpu().numpy(), ref.values(*a, ref.MX, K), ref.values(*w, ref.MX, K).reshape(G, N, K)
+    for g in range(G):      # multiples of 1/4 that fp32 holds
+        np.testing.assert_array_equal(got[off[g]:off[g + 1]], (av[off[g]:off[g + 1]] @ wv[g].T).astype(np.float32))
+    assert B.bnn_device_status() == 0
+
+
 def test_offsets_that_make_no_sense_stay_inside(env):
     torch, B = env
     rng = np.random.default_rng(1)
