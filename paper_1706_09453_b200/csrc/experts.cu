@@ -2,12 +2,13 @@
 //
 // Router: the k largest logits of a token (ties: the lowest expert), their softmax weights, and a counting sort of the T * k
 // (token, expert) pairs by expert, stable in the token: slot = offsets[expert] + how many earlier tokens chose it.  A warp takes a
-// token, its logits in registers as ordered integers; a pick is a warp maximum.  Within a block's tokens an expert has a
+// token, its logits in registers as ordered integers; a pick is a maximum over the warp.  Within a block's tokens an expert has a
 // bit mask of the tokens that chose it, so that a rank is a popcount and no order of atomics can change a result.  Up to
 // kOneBlock tokens one block does it all; beyond, a first kernel chooses and counts by block, and a second one adds the
-// counts of the blocks before (behind a kernel that sums them, where there are many) and places.  16384 tokens, 256 experts, eight
-// each, fp32: 22 us, 14 of them the choice (650 instructions of a warp per token; the logits' 17 MB are 2.6 us); 8 tokens, 64
-// experts: 3.4 us.
+// counts of the blocks before (behind a kernel that sums them, where there are many) and places.  Bound by the instructions and the
+// latency of the picks, one maximum over the warp after the other: 16384 tokens, 256 experts, eight each, take 16.4 us in bf16 and 20.6 in
+// fp32, 5 of them the places (the logits' 8 or 17 MB are 1.3 or 2.6).  2.7 of the 20.6 are one or two tokens with logits that agree in 29
+// bits.  8 tokens, 64 experts: 3 us.
 //
 // Weighted sum: bound by memory, 8192 tokens with four rows of 4096 bf16 each 53.5 us (6.3 TB/s).
 #include <cuda_bf16.h>
@@ -30,16 +31,12 @@ __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__half* p, float v) { *p = __float2half_rn(v); }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// fp32 <-> unsigned in the same order; 0 stands for "not to be chosen" (-inf, NaN).  -0 is made +0 first: they tie.
+// fp32 -> unsigned in the same order; 0 stands for "not to be chosen" (-inf, NaN).  -0 is made +0 first: they tie.
 __device__ __forceinline__ uint32_t key_of(float x) {
     if (!(x > -INFINITY)) return 0u;
     const uint32_t b = __float_as_uint(x + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float value_of(uint32_t key) {
-    return key & 0x80000000u ? __uint_as_float(key & 0x7FFFFFFFu) : __uint_as_float(~key);
-}
-
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
@@ -58,35 +55,107 @@ struct Args {
     int summed;
 };
 
-// exp(x) for x <= 0, within a few 2^-22.
+// exp(x) for x <= 0 or just above, within a few 2^-22.
 __device__ __forceinline__ float fast_exp(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.44269504f));
     return r;
 }
 
-// A lane's two largest keys among those not yet taken (a bit each), and which they are; of equal keys the lowest comes first.
+// The k best of a warp's logits by their full keys: lane j < k gets the j-th one's expert (-1: none).  A pick is the first behind
+// the one before it in the order of (key down, expert up).
 template <int V>
-__device__ __forceinline__ void best_two(const uint32_t (&key)[V], uint32_t taken, uint32_t* best, int* at, uint32_t* second, int* at2) {
-    uint32_t b = 0u, s = 0u;
-    int a = 0, a2 = 0;
+__device__ __forceinline__ int pick_exact(const float (&f)[V], int k, int lane) {
+    int expert = -1, last = -1;
+    uint32_t limit = 0xFFFFFFFFu;
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {
+        uint32_t best = 0u;
+        int at = 0x7FFFFFFF;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const uint32_t x = taken >> v & 1u ? 0u : key[v];
-        const bool first = x > b, next = x > s;
-        s = first ? b : next ? x : s;
-        a2 = first ? a : next ? v : a2;
-        b = first ? x : b;
-        a = first ? v : a;
+        for (int v = 0; v < V; ++v) {
+            const uint32_t key = key_of(f[v]);
+            const int e = v * 32 + lane;
+            if (key > best && (key < limit || (key == limit && e > last))) {
+                best = key;
+                at = e;
+            }
+        }
+        limit = __reduce_max_sync(0xFFFFFFFFu, best);
+        if (limit == 0u) break;
+        last = (int)__reduce_min_sync(0xFFFFFFFFu, best == limit ? (unsigned)at : 0xFFFFFFFFu);
+        if (lane == j) expert = last;
     }
-    *best = b; *at = a; *second = s; *at2 = a2;
+    return expert;
 }
 
-// A warp's token: lane j < k keeps the j-th choice (-1: none) and its weight.  A pick is the maximum of the lanes' best keys; the
-// lane that had it goes on with its second best, and looks for the one after only when that is picked as well.
+__device__ __forceinline__ void keep_three(uint32_t x, uint32_t& a, uint32_t& b, uint32_t& c) {
+    c = max(c, min(b, x));
+    b = max(b, min(a, x));
+    a = max(a, x);
+}
+
+// The same on words that hold the upper bits of a key and, in the lower ones, V - 1 - v, so that a lane's are all different and of equal
+// upper bits the lowest expert comes first (across lanes: the lowest lane).  A pick is the maximum of the lanes' best
+// words; the lane that had it goes on with its second and third, and looks for more only behind those.  WHOLE: the
+// upper bits are all of the key that can differ.  Otherwise the answer tells whether picks with the same upper bits may be out of
+// order (1), or the last of them have the same as one that was not picked (2).
+template <int V, bool WHOLE>
+__device__ __forceinline__ int pick_packed(const float (&f)[V], const uint32_t (&word)[V], uint32_t a, uint32_t b, uint32_t c, int k, int lane, int* expert) {
+    constexpr uint32_t LOW = V - 1;            // V is a power of two
+    uint32_t mine = 0u;
+    int left = 3, chosen = -1;
+    for (int j = 0; j < k; ++j) {
+        const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, a);
+        if (most == 0u) break;
+        const int winner = __ffs(__ballot_sync(0xFFFFFFFFu, a == most)) - 1;
+        if (lane == j) {
+            mine = most;
+            chosen = (int)(LOW - (most & LOW)) * 32 + winner;
+        }
+        const bool had = lane == winner;
+        a = had ? b : a;
+        b = had ? c : b;
+        left -= had;
+        if (left == 0) {
+            a = b = c = 0u;
+#pragma unroll
+            for (int v = 0; v < V; ++v) keep_three(word[v] < most ? word[v] : 0u, a, b, c);
+            left = 3;
+        }
+    }
+    *expert = chosen;
+    if (WHOLE) return 0;
+    const uint32_t rest = __reduce_max_sync(0xFFFFFFFFu, a);
+    uint32_t next = __shfl_down_sync(0xFFFFFFFFu, mine, 1);
+    if (lane == k - 1) next = rest;
+    const unsigned same = __ballot_sync(0xFFFFFFFFu, lane < k && mine && next && (mine ^ next) <= LOW);
+    return same == 0u ? 0 : same >> (k - 1) ? 2 : 1;
+}
+
+// The picks in the order of (logit down, expert up).  (A token in ten thousand comes here: short code, which is not at hand.)
+__device__ __noinline__ int in_order(float x, int expert, int k, int lane) {
+    int rank = 0;
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {
+        const float y = __shfl_sync(0xFFFFFFFFu, x, j);
+        const int e = __shfl_sync(0xFFFFFFFFu, expert, j);
+        rank += e >= 0 && (expert < 0 || y > x || (y == x && e < expert)) ? 1 : 0;
+    }
+    if (expert < 0) rank = lane;
+    int mine = -1;
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {
+        const unsigned who = __ballot_sync(0xFFFFFFFFu, lane < k && rank == j);
+        const int e = __shfl_sync(0xFFFFFFFFu, expert, __ffs(who) - 1);
+        if (lane == j) mine = e;
+    }
+    return mine;
+}
+
+// A warp's token: lane j < k keeps the j-th choice (-1: none) and its weight.
 template <typename T, int V>
 __device__ __forceinline__ int choose(const T* x, const Args& g, int lane, float* weight) {
-    uint32_t key[V];
     float f[V];
     bool bad = false;
 #pragma unroll
@@ -95,53 +164,34 @@ __device__ __forceinline__ int choose(const T* x, const Args& g, int lane, float
         f[v] = e < g.E ? to_f32(x[e]) : -INFINITY;
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        bad |= f[v] != f[v];
-        key[v] = key_of(f[v]);
-    }
+    for (int v = 0; v < V; ++v) bad |= f[v] != f[v];
     bad = __any_sync(0xFFFFFFFFu, bad);
-    uint32_t best, second, taken = 0u;
-    int at, at2;
-    best_two<V>(key, 0u, &best, &at, &second, &at2);
-    bool fresh = true;                 // `second` is known
-    float total = 0.0f, first = 0.0f;
-    uint32_t kept = 0u;
-    int expert = -1;
-    for (int j = 0; j < g.k; ++j) {
-        const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
-        if (most == 0u) break;
-        if (j == 0) {
-            first = value_of(most);
-            if (g.mode == BNN_ROUTE_SOFTMAX) {
-                // (the terms' errors, a few 2^-22 of each, do not add up in one direction)
-                float part = 0.0f;
+    uint32_t word[V], a = 0u, b = 0u, c = 0u;
 #pragma unroll
-                for (int v = 0; v < V; ++v) part += fast_exp(f[v] - first);
-                total = warp_sum(part);
-            }
-        }
-        const unsigned who = __ballot_sync(0xFFFFFFFFu, best == most);
-        int e = at * 32 + lane;
-        if (who & (who - 1u)) e = (int)__reduce_min_sync(0xFFFFFFFFu, best == most ? (unsigned)e : 0xFFFFFFFFu);   // a tie
-        else e = __shfl_sync(0xFFFFFFFFu, e, __ffs(who) - 1);
-        if (lane == j) {
-            kept = most;
-            expert = e;
-        }
-        if (lane == (e & 31)) {
-            taken |= 1u << at;
-            if (fresh) {
-                best = second;
-                at = at2;
-                fresh = false;
-            } else {
-                best_two<V>(key, taken, &best, &at, &second, &at2);
-                fresh = true;
-            }
-        }
+    for (int v = 0; v < V; ++v) {
+        const uint32_t y = __float_as_uint(f[v] + 0.0f), key = y ^ ((uint32_t)((int)y >> 31) | 0x80000000u);
+        word[v] = f[v] > -INFINITY ? (key & ~(V - 1u)) | (V - 1u - v) : 0u;
+        keep_three(word[v], a, b, c);
     }
-    const float part = expert >= 0 ? expf(value_of(kept) - first) : 0.0f;
-    if (g.mode == BNN_ROUTE_SOFTMAX_CHOSEN) total = warp_sum(part);
+    // A softmax may be taken from any point near the largest logit: that of the largest word, which is known before the picks.
+    const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, a);
+    const float from = most == 0u ? 0.0f : most & 0x80000000u ? __uint_as_float(most & 0x7FFFFFFFu & ~(V - 1u)) : __uint_as_float(~most | (V - 1u));
+    float total = 0.0f;
+    if (g.mode == BNN_ROUTE_SOFTMAX) {
+        // (the terms' errors do not add up in one direction)
+#pragma unroll
+        for (int v = 0; v < V; ++v) total += fast_exp(f[v] - from);
+    }
+    int expert = -1;
+    // (fp32 of a 16-bit type ends in 13 zeros or, inverted, ones: its words hold the whole key)
+    const int doubt = pick_packed<V, sizeof(T) == 2>(f, word, a, b, c, g.k, lane, &expert);
+    float logit = expert >= 0 ? to_f32(x[expert]) : -INFINITY;
+    if (doubt) {
+        expert = doubt == 1 ? in_order(logit, expert, g.k, lane) : pick_exact<V>(f, g.k, lane);
+        logit = expert >= 0 ? to_f32(x[expert]) : -INFINITY;
+    }
+    const float part = expert >= 0 ? expf(logit - from) : 0.0f;
+    total = warp_sum(g.mode == BNN_ROUTE_SOFTMAX ? total : part);
     *weight = expert < 0 ? 0.0f : bad ? __uint_as_float(0x7FC00000u) : part / total;
     return expert;
 }
