@@ -174,8 +174,11 @@ __device__ __forceinline__ int choose(const T* x, const Args& g, int lane, float
         keep_three(word[v], a, b, c);
     }
     // A softmax may be taken from any point near the largest logit: that of the largest word, which is known before the picks.
+    // A 16-bit type's is exact (its fp32 ends in 13 zeros: words hold the whole key).  fp32's is within 31 steps, which are less
+    // than two below 2^20; beyond (finite masks, say) the first pick is taken below.
+    constexpr bool WHOLE = sizeof(T) == 2;
     const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, a);
-    const float from = most == 0u ? 0.0f : most & 0x80000000u ? __uint_as_float(most & 0x7FFFFFFFu & ~(V - 1u)) : __uint_as_float(~most | (V - 1u));
+    float from = most == 0u ? 0.0f : __uint_as_float((most & 0x80000000u ? most & 0x7FFFFFFFu : ~most) & ~(V - 1u));
     float total = 0.0f;
     if (g.mode == BNN_ROUTE_SOFTMAX) {
         // (the terms' errors do not add up in one direction)
@@ -183,12 +186,20 @@ __device__ __forceinline__ int choose(const T* x, const Args& g, int lane, float
         for (int v = 0; v < V; ++v) total += fast_exp(f[v] - from);
     }
     int expert = -1;
-    // (fp32 of a 16-bit type ends in 13 zeros or, inverted, ones: its words hold the whole key)
-    const int doubt = pick_packed<V, sizeof(T) == 2>(f, word, a, b, c, g.k, lane, &expert);
+    const int doubt = pick_packed<V, WHOLE>(f, word, a, b, c, g.k, lane, &expert);
     float logit = expert >= 0 ? to_f32(x[expert]) : -INFINITY;
-    if (doubt) {
-        expert = doubt == 1 ? in_order(logit, expert, g.k, lane) : pick_exact<V>(f, g.k, lane);
-        logit = expert >= 0 ? to_f32(x[expert]) : -INFINITY;
+    const bool coarse = !WHOLE && V > 1 && fabsf(from) >= 1048576.0f;
+    if (doubt || coarse) {
+        if (doubt) {
+            expert = doubt == 1 ? in_order(logit, expert, g.k, lane) : pick_exact<V>(f, g.k, lane);
+            logit = expert >= 0 ? to_f32(x[expert]) : -INFINITY;
+        }
+        if (coarse) {
+            from = __shfl_sync(0xFFFFFFFFu, logit, 0);
+            total = 0.0f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) total += fast_exp(f[v] - from);
+        }
     }
     const float part = expert >= 0 ? expf(logit - from) : 0.0f;
     total = warp_sum(g.mode == BNN_ROUTE_SOFTMAX ? total : part);

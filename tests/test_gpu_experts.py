@@ -83,6 +83,28 @@ def test_logits_that_differ_in_their_last_bits(env, E):
     check_route(torch, B, torch.as_tensor(h, device=DEV), k)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("E", [20, 33, 100, 200, 500, 1000])
+def test_logits_of_large_size(env, dtype, E):
+    """Rows of masks (finite ones: -1e4, -1e9, the type's lowest value), whole and in part, and logits far above one."""
+    torch, B = env
+    t = dtype_of(torch, dtype)
+    top = torch.finfo(t).max
+    g = torch.Generator(device=DEV)
+    g.manual_seed(E)
+    rows = []
+    for size in (1e4, 5e4, 1048575.0, 1048577.0, 1e9, 1.2345e30, top):
+        if size > top:
+            continue
+        for sign in (1.0, -1.0):
+            flat = torch.full((4, E), sign * size, device=DEV)
+            flat[1, E // 2:] = 0.0
+            flat[2, ::3] = torch.randn((1, flat[2, ::3].numel()), generator=g, device=DEV)[0]
+            flat[3] *= 1.0 - torch.randint(0, 32, (E,), generator=g, device=DEV) * 2.0 ** -24       # steps apart
+            rows.append(flat)
+    check_route(torch, B, torch.cat(rows).to(t), min(E, 6))
+
+
 def test_nan_and_infinity(env):
     torch, B = env
     x = torch.randn((6, 20), device=DEV)
