@@ -6,7 +6,7 @@
 // bit mask of the tokens that chose it, so that a rank is a popcount and no order of atomics can change a result.  Up to
 // kOneBlock tokens one block does it all; beyond, a first kernel chooses and counts by block, and a second one adds the
 // counts of the blocks before (behind a kernel that sums them, where there are many) and places.  Bound by the instructions and the
-// latency of the picks, one maximum over the warp after the other: 16384 tokens, 256 experts, eight each, take 16.4 us in bf16 and 20.6 in
+// latency of the picks, one maximum over the warp after the other: 16384 tokens, 256 experts, eight each, take 16.7 us in bf16 and 20.6 in
 // fp32, 5 of them the places (the logits' 8 or 17 MB are 1.3 or 2.6).  2.7 of the 20.6 are one or two tokens with logits that agree in 29
 // bits.  8 tokens, 64 experts: 3 us.
 //
