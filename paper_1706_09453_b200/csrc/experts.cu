@@ -6,9 +6,8 @@
 // bit mask of the tokens that chose it, so that a rank is a popcount and no order of atomics can change a result.  Up to
 // kOneBlock tokens one block does it all; beyond, a first kernel chooses and counts by block, and a second one adds the
 // counts of the blocks before (behind a kernel that sums them, where there are many) and places.  Bound by the instructions and the
-// latency of the picks, one maximum over the warp after the other: 16384 tokens, 256 experts, eight each, take 16.7 us in bf16 and 20.6 in
-// fp32, 5 of them the places (the logits' 8 or 17 MB are 1.3 or 2.6).  2.7 of the 20.6 are one or two tokens with logits that agree in 29
-// bits.  8 tokens, 64 experts: 3 us.
+// latency of the picks, one maximum over the warp after the other: 16384 tokens, 256 experts, eight each, take 16.6 us in bf16 and 17.3 in
+// fp32, 5 of them the places (the logits' 8 or 17 MB are 1.3 or 2.6).  8 tokens, 64 experts: 3 us.
 //
 // Weighted sum: bound by memory, 8192 tokens with four rows of 4096 bf16 each 53.5 us (6.3 TB/s).
 #include <cuda_bf16.h>
@@ -62,20 +61,20 @@ __device__ __forceinline__ float fast_exp(float x) {
     return r;
 }
 
-// The k best of a warp's logits by their full keys: lane j < k gets the j-th one's expert (-1: none).  A pick is the first behind
-// the one before it in the order of (key down, expert up).
-template <int V>
-__device__ __forceinline__ int pick_exact(const float (&f)[V], int k, int lane) {
-    int expert = -1, last = -1;
-    uint32_t limit = 0xFFFFFFFFu;
+// Choices from place j on by their full keys, of the logits whose keys are at most `limit`: lane j gets the j-th one's expert (-1:
+// none).  A pick is the first behind the one before it in the order of (key down, expert up).  (Short code, not at hand
+// when a token in ten thousand comes here: loops that read the logits again.)
+template <typename T>
+__device__ __noinline__ int pick_exact(const T* x, int E, int j, int k, uint32_t limit, int expert, int lane) {
+    int last = -1;
+    if (lane >= j) expert = -1;
 #pragma unroll 1
-    for (int j = 0; j < k; ++j) {
+    for (; j < k; ++j) {
         uint32_t best = 0u;
         int at = 0x7FFFFFFF;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t key = key_of(f[v]);
-            const int e = v * 32 + lane;
+#pragma unroll 1
+        for (int e = lane; e < E; e += 32) {
+            const uint32_t key = key_of(to_f32(x[e]));
             if (key > best && (key < limit || (key == limit && e > last))) {
                 best = key;
                 at = e;
@@ -98,10 +97,10 @@ __device__ __forceinline__ void keep_three(uint32_t x, uint32_t& a, uint32_t& b,
 // The same on words that hold the upper bits of a key and, in the lower ones, V - 1 - v, so that a lane's are all different and of equal
 // upper bits the lowest expert comes first (across lanes: the lowest lane).  A pick is the maximum of the lanes' best
 // words; the lane that had it goes on with its second and third, and looks for more only behind those.  WHOLE: the
-// upper bits are all of the key that can differ.  Otherwise the answer tells whether picks with the same upper bits may be out of
-// order (1), or the last of them have the same as one that was not picked (2).
+// upper bits are all of the key that can differ.  Otherwise the answer has a bit for every pick whose upper bits are those of the
+// next one, which may be before it, or (the last) of one that was not picked.
 template <int V, bool WHOLE>
-__device__ __forceinline__ int pick_packed(const float (&f)[V], const uint32_t (&word)[V], uint32_t a, uint32_t b, uint32_t c, int k, int lane, int* expert) {
+__device__ __forceinline__ unsigned pick_packed(const uint32_t (&word)[V], uint32_t a, uint32_t b, uint32_t c, int k, int lane, int* expert, uint32_t* picked) {
     constexpr uint32_t LOW = V - 1;            // V is a power of two
     uint32_t mine = 0u;
     int left = 3, chosen = -1;
@@ -125,12 +124,12 @@ __device__ __forceinline__ int pick_packed(const float (&f)[V], const uint32_t (
         }
     }
     *expert = chosen;
-    if (WHOLE) return 0;
+    *picked = mine;
+    if (WHOLE) return 0u;
     const uint32_t rest = __reduce_max_sync(0xFFFFFFFFu, a);
     uint32_t next = __shfl_down_sync(0xFFFFFFFFu, mine, 1);
     if (lane == k - 1) next = rest;
-    const unsigned same = __ballot_sync(0xFFFFFFFFu, lane < k && mine && next && (mine ^ next) <= LOW);
-    return same == 0u ? 0 : same >> (k - 1) ? 2 : 1;
+    return __ballot_sync(0xFFFFFFFFu, lane < k && mine && next && (mine ^ next) <= LOW);
 }
 
 // The picks in the order of (logit down, expert up).  (A token in ten thousand comes here: short code, which is not at hand.)
@@ -186,19 +185,27 @@ __device__ __forceinline__ int choose(const T* x, const Args& g, int lane, float
         for (int v = 0; v < V; ++v) total += fast_exp(f[v] - from);
     }
     int expert = -1;
-    const int doubt = pick_packed<V, WHOLE>(f, word, a, b, c, g.k, lane, &expert);
+    uint32_t picked;
+    const unsigned doubt = pick_packed<V, WHOLE>(word, a, b, c, g.k, lane, &expert, &picked);
     float logit = expert >= 0 ? to_f32(x[expert]) : -INFINITY;
     const bool coarse = !WHOLE && V > 1 && fabsf(from) >= 1048576.0f;
     if (doubt || coarse) {
-        if (doubt) {
-            expert = doubt == 1 ? in_order(logit, expert, g.k, lane) : pick_exact<V>(f, g.k, lane);
+        if (doubt >> (g.k - 1)) {
+            // the last of them anew: those of the last one's upper bits
+            const uint32_t upper = __shfl_sync(0xFFFFFFFFu, picked, g.k - 1) | (V - 1u);
+            const int from_place = __ffs(__ballot_sync(0xFFFFFFFFu, (picked | (V - 1u)) == upper)) - 1;
+            expert = pick_exact(x, g.E, from_place, g.k, upper, expert, lane);
+            logit = expert >= 0 ? to_f32(x[expert]) : -INFINITY;
+        }
+        if (doubt & ((1u << (g.k - 1)) - 1u)) {
+            expert = in_order(logit, expert, g.k, lane);
             logit = expert >= 0 ? to_f32(x[expert]) : -INFINITY;
         }
         if (coarse) {
             from = __shfl_sync(0xFFFFFFFFu, logit, 0);
             total = 0.0f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) total += fast_exp(f[v] - from);
+#pragma unroll 1
+            for (int e = lane; e < g.E; e += 32) total += fast_exp(to_f32(x[e]) - from);
         }
     }
     const float part = expert >= 0 ? expf(logit - from) : 0.0f;
