@@ -6,7 +6,7 @@
 // bit mask of the tokens that chose it, so that a rank is a popcount and no order of atomics can change a result.  Up to
 // kOneBlock tokens one block does it all; beyond, a first kernel chooses and counts by block, and a second one adds the
 // counts of the blocks before (behind a kernel that sums them, where there are many) and places.  Bound by the instructions and the
-// latency of the picks, one maximum over the warp after the other: 16384 tokens, 256 experts, eight each, take 16.6 us in bf16 and 17.3 in
+// latency of the picks, one maximum over the warp after the other: 16384 tokens, 256 experts, eight each, take 16.8 us in bf16 and 16.8 in
 // fp32, 5 of them the places (the logits' 8 or 17 MB are 1.3 or 2.6).  8 tokens, 64 experts: 3 us.
 //
 // Weighted sum: bound by memory, 8192 tokens with four rows of 4096 bf16 each 53.5 us (6.3 TB/s).
@@ -256,10 +256,11 @@ __device__ __forceinline__ void place(const Args& g, const uint16_t* index, cons
 __device__ __forceinline__ int* numbers_of(uint32_t* mask, const Args& g) { return reinterpret_cast<int*>(mask + g.E * g.words); }
 __device__ __forceinline__ uint16_t* pairs_of(uint32_t* mask, const Args& g) { return reinterpret_cast<uint16_t*>(mask + g.E * (g.words + 2)); }
 
+// (The router's kernels do not let the next one start early: its blocks would wait beside the ones at work.  4096 tokens, 512 experts, eight
+// each 16.6 us with a trigger at the start, 12.1 without; 8192, 64, two 11.5 and 8.4; 16384, 256, eight, with one behind the choice 27, without 16.8.)
 template <typename T, int V>
 __global__ void __launch_bounds__(THREADS) choose_kernel(const __grid_constant__ Args g) {
     extern __shared__ uint32_t mask[];
-    pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint16_t* pairs = pairs_of(mask, g);
     for (int i = threadIdx.x; i < g.E * g.words; i += THREADS) mask[i] = 0u;
@@ -295,7 +296,6 @@ __global__ void __launch_bounds__(THREADS) choose_kernel(const __grid_constant__
 // sums[b][e]: the counts of the blocks before b, and behind them those of all; 32 experts a block, its warps share the blocks.
 __global__ void __launch_bounds__(THREADS) sum_kernel(const __grid_constant__ Args g) {
     __shared__ int part[WARPS][33];
-    pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
     const int each = ceil_div(g.blocks, WARPS), lo = min(warp * each, g.blocks), hi = min(lo + each, g.blocks);
@@ -317,7 +317,6 @@ __global__ void __launch_bounds__(THREADS) sum_kernel(const __grid_constant__ Ar
 
 __global__ void __launch_bounds__(THREADS) place_kernel(const __grid_constant__ Args g) {
     extern __shared__ uint32_t mask[];
-    pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int* base = numbers_of(mask, g);
     int* total = base + g.E;
