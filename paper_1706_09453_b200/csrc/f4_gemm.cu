@@ -66,6 +66,7 @@ struct Args {
     const float* scale;
     const float* shift;
     int act, sign_mode, box, split, tile_rows;
+    int early;              // the next kernel may start while this one runs
     void* Y;
     int dtype, pieces;
     long long ldy;
@@ -223,7 +224,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
     constexpr int OUT_AT = S::STAGES * S::STAGE;
     Control* ctl = reinterpret_cast<Control*>(smem + OUT_AT + S::OUT_BYTES);
     volatile int* abort_flag = &ctl->wait.abort;
-    pdl_trigger();
+    if (g.early) pdl_trigger();
     const int warp = warp_index(), lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)cluster_rank() : 0, part = SPLIT ? (int)cluster_rank() : 0;
     constexpr int CTAS = PAIR ? 2 : 1;
@@ -630,6 +631,10 @@ int launch_form(const F4GemmArgs& a, Args g, int tile_rows, int box, int sms, cu
     else kern = f4_gemm_kernel<MX, TN, SPLIT>;
     if (!ensure_dynamic_smem(reinterpret_cast<const void*>(kern), S::SMEM) || !encode_maps<S>(&maps, a, g.kt, box)) return BNN_ERR_CUDA;
     const long long tiles = tiles_of(a, tile_rows, BM * CTAS);
+    // The next kernel's blocks beside this one's are worth it where every SM has one tile at most (one token 5.2 us, and 5.6 where
+    // they come at the end); beside many turns they only get in each other's way (quantisation and product, 8192 x 2048 x 2048: 29.4, and
+    // 27.6 at the end).
+    g.early = tiles <= sms / CTAS;
     if constexpr (SPLIT) {
         if (launch_pdl_cluster(kern, dim3((unsigned)(tiles * g.split)), dim3(THREADS), g.split, S::SMEM, st, maps, g) != cudaSuccess) return BNN_ERR_CUDA;
     } else {
