@@ -555,12 +555,14 @@ def _flat(t, dtype, n, what):
     return t.data_ptr()
 
 
-def _codes(t, dim=2):
-    """(address, pitch) of rows of codes"""
+def _codes(t, k, dim=2):
+    """(address, pitch) of rows of codes.  Kernels take all bytes of a row that K elements need: of rows that are shorter (columns of
+    a wider tensor, say) the call is told the length instead, and refuses it."""
     stride = t.stride()
     if t.dtype is not torch.uint8 or len(stride) != dim or stride[-1] != 1:
         _refuse("codes: expected a %d-D uint8 tensor with contiguous rows" % dim)
-    return t.data_ptr(), stride[-2]
+    width = t.shape[-1]
+    return t.data_ptr(), stride[-2] if width >= (k + 31) // 32 * 16 else width
 
 
 def _scales(t):
@@ -592,7 +594,7 @@ def bnn_f4_quantize(X, codes, scales, fmt=F4_E8M0_32, source=None, offsets=None,
     _here((X, codes, scales, source, offsets))
     rows, (src_rows, k) = codes.shape[0], X.shape
     src = 0 if source is None else _flat(source, torch.int32, rows, "source")
-    _f4_quantize(X.data_ptr(), _dtype(X), src_rows, k, _ld(X), src, *_groups(offsets), rows, fmt, exponent, *_codes(codes),
+    _f4_quantize(X.data_ptr(), _dtype(X), src_rows, k, _ld(X), src, *_groups(offsets), rows, fmt, exponent, *_codes(codes, k),
                  *_scales(scales), _stream())
     return codes, scales
 
@@ -603,19 +605,19 @@ def bnn_f4_dequantize(codes, scales, Y, fmt=F4_E8M0_32, offsets=None, exponent=0
     rows, k = Y.shape
     if codes.shape[0] != rows:
         _refuse("codes and Y have different numbers of rows")
-    _f4_dequantize(*_codes(codes), *_scales(scales), *_groups(offsets), rows, k, fmt, exponent, Y.data_ptr(), _dtype(Y), _ld(Y), _stream())
+    _f4_dequantize(*_codes(codes, k), *_scales(scales), *_groups(offsets), rows, k, fmt, exponent, Y.data_ptr(), _dtype(Y), _ld(Y), _stream())
     return Y
 
 
-def _f4_epilogue(rows, n, act, sign_mode, scale, shift, out_bits):
-    """The epilogue of a product; None where there is nothing to it."""
+def _f4_epilogue(rows, groups, n, act, sign_mode, scale, shift, out_bits):
+    """The epilogue of a product of n units a group; None where there is nothing to it."""
     if act == ACT_NONE and scale is None and shift is None and out_bits is None:
         return None
     for t in (scale, shift):
         if t is not None:
-            _flat(t, torch.float32, n, "scale, shift")
-    if out_bits is not None and out_bits.shape[0] != rows:
-        _refuse("out_bits has another number of rows")
+            _flat(t, torch.float32, groups * n, "scale, shift")
+    if out_bits is not None and (out_bits.dim() != 2 or out_bits.shape[0] != rows or out_bits.shape[1] < (n + 31) // 32):
+        _refuse("out_bits: expected %d rows of at least %d words" % (rows, (n + 31) // 32))
     return _epilogue(act, sign_mode, scale, shift, out_bits=out_bits)
 
 
@@ -633,8 +635,8 @@ def bnn_f4_gemm(A, a_scales, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0,
     """Y = act(fma(2^exponent * scale, A W^T, shift)) of two quantised matrices (codes uint8 [rows][pitch], scales)."""
     _here((A, a_scales, W, w_scales, Y, scale, shift, out_bits))
     m, n = A.shape[0], W.shape[0]
-    e = _f4_epilogue(m, n, act, sign_mode, scale, shift, out_bits)
-    _f4_gemm(*_codes(A), *_scales(a_scales), *_codes(W), *_scales(w_scales), m, n, K, fmt, exponent, *_f4_result(Y, m, n),
+    e = _f4_epilogue(m, 1, n, act, sign_mode, scale, shift, out_bits)
+    _f4_gemm(*_codes(A, K), *_scales(a_scales), *_codes(W, K), *_scales(w_scales), m, n, K, fmt, exponent, *_f4_result(Y, m, n),
              0 if e is None else C.addressof(e), _stream())
     return Y if out_bits is None else out_bits
 
@@ -648,8 +650,8 @@ def bnn_f4_gemm_grouped(A, a_scales, offsets, W, w_scales, K, Y=None, fmt=F4_E8M
     if len(shape) != 3 or shape[0] != groups or (groups > 1 and stride[0] != shape[1] * stride[1]):
         _refuse("W: expected [%d, N, pitch], the groups one behind the other" % groups)
     m, n = A.shape[0], shape[1]
-    e = _f4_epilogue(m, groups * n, act, sign_mode, scale, shift, out_bits)
-    _f4_gemm_grouped(*_codes(A), *_scales(a_scales), off, groups, *_codes(W, 3), *_scales(w_scales), m, n, K, fmt, exponent,
+    e = _f4_epilogue(m, groups, n, act, sign_mode, scale, shift, out_bits)
+    _f4_gemm_grouped(*_codes(A, K), *_scales(a_scales), off, groups, *_codes(W, K, 3), *_scales(w_scales), m, n, K, fmt, exponent,
                      *_f4_result(Y, m, n), 0 if e is None else C.addressof(e), _stream())
     return Y if out_bits is None else out_bits
 
