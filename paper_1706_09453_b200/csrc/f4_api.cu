@@ -12,6 +12,8 @@ using namespace bnn;
 namespace {
 
 constexpr int kMaxExponent = 64, kMaxChoices = 32;
+// Rows, tokens and columns are rounded up to whole blocks (4096 columns at most) in 32 bits.
+constexpr int kMaxLength = 0x7FFFFFFF - 4096;
 
 bool known_format(int f) { return f == BNN_F4_E8M0_32 || f == BNN_F4_E4M3_16; }
 bool known_dtype(int d) { return d == BNN_DTYPE_F32 || d == BNN_DTYPE_F16 || d == BNN_DTYPE_BF16; }
@@ -128,7 +130,7 @@ int bnn_f4_quantize(const void* X, int dtype, int src_rows, int K, int ldx, cons
                     int rows, int format, int exponent, void* codes, int ldc, void* scales, size_t scale_bytes, void* stream) {
     if (!X) return BNN_ERR_NULL;
     if (!known_format(format) || !known_dtype(dtype)) return BNN_ERR_UNSUPPORTED;
-    if (rows < 1 || src_rows < 1 || K < 1 || K > f4::kMaxK || ldx < K || (!source && src_rows < rows)) return BNN_ERR_SHAPE;
+    if (rows < 1 || rows > kMaxLength || src_rows < 1 || K < 1 || K > f4::kMaxK || ldx < K || (!source && src_rows < rows)) return BNN_ERR_SHAPE;
     if (exponent < -kMaxExponent || exponent > kMaxExponent) return BNN_ERR_SHAPE;
     if (int rc = check_groups(offsets, groups)) return rc;
     if (int rc = check_f4(codes, ldc, scales, scale_bytes, format, rows, groups, K)) return rc;
@@ -144,7 +146,7 @@ int bnn_f4_dequantize(const void* codes, int ldc, const void* scales, size_t sca
                       int K, int format, int exponent, void* Y, int dtype, int ldy, void* stream) {
     if (!Y) return BNN_ERR_NULL;
     if (!known_format(format) || !known_dtype(dtype)) return BNN_ERR_UNSUPPORTED;
-    if (rows < 1 || K < 1 || K > f4::kMaxK || ldy < K) return BNN_ERR_SHAPE;
+    if (rows < 1 || rows > kMaxLength || K < 1 || K > f4::kMaxK || ldy < K) return BNN_ERR_SHAPE;
     if (exponent < -kMaxExponent || exponent > kMaxExponent) return BNN_ERR_SHAPE;
     if (int rc = check_groups(offsets, groups)) return rc;
     if (int rc = check_f4(codes, ldc, scales, scale_bytes, format, rows, groups, K)) return rc;
@@ -172,14 +174,14 @@ int bnn_f4_gemm_grouped(const void* A, int lda, const void* a_scales, size_t a_s
 }
 
 size_t bnn_route_workspace_bytes(int T, int E) {
-    return T < 1 || E < 1 || E > f4::kMaxGroups ? 0 : route_workspace_bytes(T, E);
+    return T < 1 || T > kMaxLength || E < 1 || E > f4::kMaxGroups ? 0 : route_workspace_bytes(T, E);
 }
 
 int bnn_route_experts(const void* logits, int dtype, int T, int E, int ld, int k, int mode, int32_t* index, float* weight,
                       int32_t* offsets, int32_t* slot, int32_t* source, void* workspace, size_t workspace_bytes, void* stream) {
     if (!logits || !index || !weight || !offsets || !slot || !source) return BNN_ERR_NULL;
     if (!known_dtype(dtype) || (mode != BNN_ROUTE_SOFTMAX && mode != BNN_ROUTE_SOFTMAX_CHOSEN)) return BNN_ERR_UNSUPPORTED;
-    if (T < 1 || E < 1 || E > f4::kMaxGroups || ld < E || k < 1 || k > E || k > kMaxChoices || T > 0x7FFFFFFF / k) return BNN_ERR_SHAPE;
+    if (T < 1 || T > kMaxLength || E < 1 || E > f4::kMaxGroups || ld < E || k < 1 || k > E || k > kMaxChoices || T > 0x7FFFFFFF / k) return BNN_ERR_SHAPE;
     if (!aligned_to(logits, size_of(dtype)) || !aligned_to(index, 4) || !aligned_to(weight, 4) || !aligned_to(offsets, 4) ||
         !aligned_to(slot, 4) || !aligned_to(source, 4) || !aligned16(workspace))
         return BNN_ERR_ALIGN;
@@ -194,7 +196,7 @@ int bnn_combine_experts(const void* Z, int z_dtype, int rows, int ldz, const int
                         void* Y, int y_dtype, int ldy, void* stream) {
     if (!Z || !slot || !weight || !Y) return BNN_ERR_NULL;
     if (!known_dtype(z_dtype) || !known_dtype(y_dtype)) return BNN_ERR_UNSUPPORTED;
-    if (rows < 1 || T < 1 || k < 1 || k > kMaxChoices || N < 1 || ldz < N || ldy < N) return BNN_ERR_SHAPE;
+    if (rows < 1 || T < 1 || k < 1 || k > kMaxChoices || N < 1 || N > kMaxLength || ldz < N || ldy < N) return BNN_ERR_SHAPE;
     if (!aligned_to(Z, size_of(z_dtype)) || !aligned_to(Y, size_of(y_dtype)) || !aligned_to(slot, 4) || !aligned_to(weight, 4))
         return BNN_ERR_ALIGN;
     CombineArgs a{};
