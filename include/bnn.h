@@ -544,7 +544,8 @@ BNN_API int bnn_f4_dequantize(const void* codes, int ldc, const void* scales, si
  * binary layer).  Any M from one row on.
  * bnn_f4_gemm_grouped: group g's rows of A by W's rows g * N .. g * N + N - 1; W is [groups * N] rows whose scales are stored with
  * offsets[g] = g * N; scale and shift are [groups][N].
- * The results may not overlap the operands.  Errors: as bnn_f4_quantize; BNN_ERR_UNSUPPORTED also for an act that is not named above. */
+ * The results may not overlap the operands.  Errors: as bnn_f4_quantize; BNN_ERR_UNSUPPORTED also for an act that is not named above and
+ * for out_bits without BNN_ACT_SIGN_PACK. */
 BNN_API int bnn_f4_gemm(const void* A, int lda, const void* a_scales, size_t a_scale_bytes,
                 const void* W, int ldw, const void* w_scales, size_t w_scale_bytes,
                 int M, int N, int K, int format, int exponent, void* Y, int dtype, int ldy,

@@ -71,6 +71,7 @@ int gemm_checked(const void* a, int lda, const void* a_scales, size_t a_scale_by
         g.ldob = epi->ldob;
     } else {
         if (g.act != BNN_ACT_NONE && g.act != BNN_ACT_HARDTANH && g.act != BNN_ACT_SIGMOID) return BNN_ERR_UNSUPPORTED;
+        if (epi && epi->out_bits) return BNN_ERR_UNSUPPORTED;      // bits are written by BNN_ACT_SIGN_PACK alone
         if (!known_dtype(dtype)) return BNN_ERR_UNSUPPORTED;
         if (!Y) return BNN_ERR_NULL;
         if (ldy < N) return BNN_ERR_SHAPE;
