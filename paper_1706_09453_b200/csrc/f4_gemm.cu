@@ -569,17 +569,24 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
     tc_fence_before_sync();
     __syncthreads();
     if (*abort_flag) {
-        // what is still on its way ends first: the MMAs and the copies (of a pair: those of both CTAs, counted on rank 0)
+        // What is still on its way ends first, whatever the limit was that ran out: the MMAs, and the copies.  Those of a pair are counted on rank
+        // 0, which may have stopped before it asked for as many as rank 1: rank 1, which cannot see that barrier, gives its own the time.  (A
+        // rank that did not give up has seen its last accumulator, and so the end of all copies.)
+        const long long until = clock64() + kDrainClocks;
         if (warp == MMA_WARP) {
             if (rank == 0 && elect_one()) {
                 if constexpr (PAIR) mma_commit_pair(smem_u32(&ctl->drained));
                 else mma_commit(smem_u32(&ctl->drained));
             }
             __syncwarp();
-            mbar_wait_out(smem_u32(&ctl->drained), 0u, g.status.limit);
-        } else if (warp == TMA_WARP && lane == 0 && rank == 0) {
-            for (int i = max(0, issued - S::STAGES); i < issued; ++i)
-                mbar_wait_out(smem_u32(&ctl->full[i % S::STAGES]), (uint32_t)(i / S::STAGES) & 1u, g.status.limit);
+            mbar_wait_out(smem_u32(&ctl->drained), 0u, until);
+        } else if (warp == TMA_WARP && lane == 0) {
+            if (rank == 0) {
+                for (int i = max(0, issued - S::STAGES); i < issued; ++i)
+                    mbar_wait_out(smem_u32(&ctl->full[i % S::STAGES]), (uint32_t)(i / S::STAGES) & 1u, until);
+            } else {
+                while (issued > 0 && clock64() < until) {}
+            }
         }
         __syncwarp();
         __syncthreads();

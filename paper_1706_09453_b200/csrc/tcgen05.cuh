@@ -76,12 +76,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     return true;
 }
 
-// The same on the way out, after another wait has run out: bounded by the clock alone.
-__device__ __forceinline__ void mbar_wait_out(uint32_t bar, uint32_t parity, long long limit) {
-    const long long t0 = clock64();
+// The same on the way out, after another wait has run out: until the clock says `until`.  The limit that has run out may be
+// the user's and short; what is on its way when a kernel gives up needs microseconds, and gets kDrainClocks (8 ms).
+constexpr long long kDrainClocks = 1ll << 24;
+__device__ __forceinline__ void mbar_wait_out(uint32_t bar, uint32_t parity, long long until) {
 #pragma unroll 1
     while (!mbar_try_wait(bar, parity))
-        if (clock64() - t0 > limit) return;
+        if (clock64() > until) return;
 }
 
 // Wait of a role that has slack (an epilogue warp waiting for a whole tile of MMAs, the thread
