@@ -509,7 +509,8 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
     }
 
     if constexpr (SPLIT) {
-        // every CTA adds up its share of the rows from all parts, a warp a row and a lane four units, its own part first
+        // every CTA adds up its share of the rows from all parts, a warp a row and a lane four units, in the order of K: a row's
+        // sum must not depend on whose share it falls into
         __syncwarp();
         cluster_sync();
         if (warp < EPI_WARPS && worker < total) {
@@ -527,7 +528,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Args& g) {
                 float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
                 for (int i = 0; i < g.split; ++i) {
-                    const float4 x = ld_cluster4(peer_addr(at, (part + i) & (g.split - 1)));
+                    const float4 x = ld_cluster4(peer_addr(at, i));
                     v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
                 }
                 uint32_t bits = 0;
