@@ -556,6 +556,13 @@ BNN_API int bnn_f4_gemm_grouped(const void* A, int lda, const void* a_scales, si
                         int M, int N, int K, int format, int exponent, void* Y, int dtype, int ldy,
                         const bnn_epilogue* epi, void* stream);
 
+/* How a product of these sizes is cut up, on a device of `sms` SMs (0: the current one); groups 0: bnn_f4_gemm, else bnn_f4_gemm_grouped with as
+ * many.  It is chosen by the sizes alone and shows in a result only by the order of its sums.  For measurements and tests; launches nothing.
+ *   ctas : CTAs that work on a tile together (1, or a pair);   rows : rows of A in a tile;   split : CTAs that share a tile's K.
+ * form : HOST.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_CUDA (sms 0 without a device). */
+typedef struct { int ctas, rows, split; } bnn_f4_form;
+BNN_API int bnn_f4_gemm_form(int M, int N, int K, int groups, int sms, bnn_f4_form* form);
+
 /* Router of a layer that is split into E experts (the paper has no counterpart).  logits : [T][ld] of
  * `dtype`.  For each token t, the k experts with the largest logits, descending, ties to the lowest expert:
  *   index [T][k]  : the experts;   weight [T][k] : fp32, softmax over all E logits (BNN_ROUTE_SOFTMAX) or over the chosen ones

@@ -145,6 +145,8 @@ def lib():
         L.bnn_f4_gemm.restype = i
         L.bnn_f4_gemm_grouped.argtypes = [p, i, p, z, p, i, p, i, p, z, i, i, i, i, i, p, i, i, C.POINTER(Epilogue), p]
         L.bnn_f4_gemm_grouped.restype = i
+        L.bnn_f4_gemm_form.argtypes = [i, i, i, i, i, C.POINTER(i)]
+        L.bnn_f4_gemm_form.restype = i
         L.bnn_route_workspace_bytes.argtypes = [i, i]
         L.bnn_route_workspace_bytes.restype = z
         L.bnn_route_experts.argtypes = [p, i, i, i, i, i, i, p, p, p, p, p, p, z, p]
@@ -654,6 +656,13 @@ def bnn_f4_gemm_grouped(A, a_scales, offsets, W, w_scales, K, Y=None, fmt=F4_E8M
     _f4_gemm_grouped(*_codes(A, K), *_scales(a_scales), off, groups, *_codes(W, K, 3), *_scales(w_scales), m, n, K, fmt, exponent,
                      *_f4_result(Y, m, n), 0 if e is None else C.addressof(e), _stream())
     return Y if out_bits is None else out_bits
+
+
+def bnn_f4_gemm_form(M, N, K, groups=0, sms=0):
+    """(CTAs that work on a tile together, rows of a tile, CTAs that share its K) of a product of these sizes; groups 0: bnn_f4_gemm."""
+    form = (C.c_int * 3)()
+    _check(lib().bnn_f4_gemm_form(int(M), int(N), int(K), int(groups), int(sms), form), "bnn_f4_gemm_form")
+    return tuple(form)
 
 
 def bnn_route_workspace_bytes(T, E) -> int:

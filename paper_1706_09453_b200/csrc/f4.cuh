@@ -87,6 +87,7 @@ struct F4GemmArgs {
     int ldob;
 };
 int launch_f4_gemm(const F4GemmArgs& a, cudaStream_t st);
+int f4_gemm_form(int M, int N, int K, int groups, int sms, bnn_f4_form* form);
 
 struct RouteArgs {
     const void* logits;

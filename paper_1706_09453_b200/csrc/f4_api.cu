@@ -174,6 +174,13 @@ int bnn_f4_gemm_grouped(const void* A, int lda, const void* a_scales, size_t a_s
                         Y, dtype, ldy, epi, stream);
 }
 
+int bnn_f4_gemm_form(int M, int N, int K, int groups, int sms, bnn_f4_form* form) {
+    if (!form) return BNN_ERR_NULL;
+    if (M < 1 || M > 0x7FFFFFFF - 512 || N < 1 || N > 0x7FFFFFFF - 256 || K < 1 || K > f4::kMaxK || groups < 0 || groups > f4::kMaxGroups || sms < 0)
+        return BNN_ERR_SHAPE;
+    return f4_gemm_form(M, N, K, groups, sms, form);
+}
+
 size_t bnn_route_workspace_bytes(int T, int E) {
     return T < 1 || T > kMaxLength || E < 1 || E > f4::kMaxGroups ? 0 : route_workspace_bytes(T, E);
 }

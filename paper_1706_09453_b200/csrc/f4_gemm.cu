@@ -622,23 +622,74 @@ bool encode_maps(Maps* m, const F4GemmArgs& a, int kt, int box) {
            encode_scale_map(&m->a_scales, a.a_scales, f4::row_tiles(a.M, a.groups), kt, S::ROW_TILES, S::KATOMS);
 }
 
+// The sizes that a form is chosen by; groups 0: a dense matrix.
+struct Sizes {
+    int M, N, K, groups;
+};
+
 // An upper bound on the tiles of a form: the groups' rows are only known on the device.
-long long tiles_of(const F4GemmArgs& a, int rows, int units) {
-    return (a.M / rows + (a.offsets ? (long long)(a.M < a.groups ? a.M : a.groups) : 1)) * ceil_div(a.N, units);
+long long tiles_of(const Sizes& z, int rows, int units) {
+    return (z.M / rows + (z.groups ? (long long)(z.M < z.groups ? z.M : z.groups) : 1)) * ceil_div(z.N, units);
 }
 
+// How a product is cut up: tiles of ctas * 128 units x tile_rows rows (of `width` in the kernel's layout), copied `box` rows at a time, their K
+// shared by `split` CTAs.
+struct Form {
+    int ctas, tile_rows, width, box, split;
+};
+
+// Up to 32 rows: clusters of 2 or 4 CTAs share a tile's K where the tiles alone leave SMs idle.  (Quantisation and product, one row,
+// us without and with: K = N = 2048 6.9 and 6.3, 4096 10.0 and 7.7, 8192 15.6 and 12.2, K = 8192 N = 2048 15.2 and 8.8.  Clusters of 8
+// wait for so many free SMs of a GPC that they lose: 10.4 at 2048.  So does adding up 128 rows and more: 256 rows of 2048 8.2 and 11.5.)
+Form few_rows(const Sizes& z, int sms) {
+    const long long tiles = tiles_of(z, 32, BM);
+    int split = 1;
+    while (split < MAX_SPLIT && tiles * split * 2 <= sms && split * 2 <= ceil_div(z.K, BK)) split *= 2;
+    return {1, 32, 32, z.M <= 16 ? 16 : 32, split};
+}
+
+// Which form.  Up to 32 rows: tiles of 32 (a group's second tile of 32 would start inside a tile of scales, so that these are 32
+// rows in all).  Else single CTAs (128 units x 128 rows), pairs of 256 units x 256 rows, or, without groups, of 192 rows (every second tile then
+// starts in the middle of a tile of scales), by the clocks that the SMs are estimated to take: the turns, what each takes as measured on
+// many turns (the epilogue's time where K is short), and the last one's epilogue.  Measured, us single / 192 / 256: 1024 rows, K = N =
+// 2048 6.8 / 8.0 / 8.1; 731 rows, N = 3307 11.1 / 9.0 / 9.4; 2048 rows 11.0 / 11.3 / 8.6; 4096 x 4096 x 4096 47.3 / 36.6 / 31.5; 4096 x 512 x
+// 4096 16.4 / 15.3 / 14.6; 16384 rows by 32 groups of 2048 x 4096 118 / 90 / 80.  (Pairs of 128 rows win nowhere.)
+// Groups of less than 128 rows on average are bound by their weights' bytes, and narrow tiles have more of them on their way: 2048
+// rows by 32 groups 19.3 and 21.2.
+Form form_of(const Sizes& z, int sms) {
+    if (z.M <= 32) return few_rows(z, sms);
+    const int rows = z.groups ? ceil_div(z.M, z.groups) : z.M;      // of a group, on average
+    const long long steps = ceil_div(z.K, BK);
+    auto clocks = [&](int tile, int ctas, long long shortest, long long step, long long more, long long last) {
+        // (half a tile for the rest of each group)
+        const long long row_tiles = z.groups ? z.M / tile + (z.groups + 1) / 2 : ceil_div(z.M, tile);
+        const long long turns = (row_tiles * ceil_div(z.N, BM * ctas) + sms / ctas - 1) / (sms / ctas), turn = steps * step + more;
+        return turns * (turn > shortest ? turn : shortest) + last;
+    };
+    if (rows >= 128 && sms >= 2) {
+        const long long single = clocks(128, 1, 3500, 753, 1450, 1900), high = clocks(256, 2, 5200, 743, 2350, 3800);
+        const long long low = z.groups ? high : clocks(192, 2, 3900, 700, 2200, 3000);
+        if (low < high && low < single) return {2, 192, PAIR_ROWS, 96, 1};
+        if (high < single) return {2, 256, PAIR_ROWS, 128, 1};
+    }
+    return {1, 128, 128, rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128, 1};
+}
+
+Sizes sizes_of(const F4GemmArgs& a) { return {a.M, a.N, a.K, a.offsets ? a.groups : 0}; }
+
 template <bool MX, bool PAIR, int TN, bool SPLIT>
-int launch_form(const F4GemmArgs& a, Args g, int tile_rows, int box, int sms, cudaStream_t st) {
+int launch_form(const F4GemmArgs& a, Args g, const Form& f, int sms, cudaStream_t st) {
     using S = Shape<MX, PAIR, TN, SPLIT>;
     constexpr int CTAS = PAIR ? 2 : 1;
     Maps maps;
-    g.box = box;
-    g.tile_rows = tile_rows;
+    g.box = f.box;
+    g.tile_rows = f.tile_rows;
+    g.split = f.split;
     void (*kern)(Maps, Args);
     if constexpr (PAIR) kern = f4_gemm_pair_kernel<MX>;
     else kern = f4_gemm_kernel<MX, TN, SPLIT>;
-    if (!ensure_dynamic_smem(reinterpret_cast<const void*>(kern), S::SMEM) || !encode_maps<S>(&maps, a, g.kt, box)) return BNN_ERR_CUDA;
-    const long long tiles = tiles_of(a, tile_rows, BM * CTAS);
+    if (!ensure_dynamic_smem(reinterpret_cast<const void*>(kern), S::SMEM) || !encode_maps<S>(&maps, a, g.kt, f.box)) return BNN_ERR_CUDA;
+    const long long tiles = tiles_of(sizes_of(a), f.tile_rows, BM * CTAS);
     // The next kernel's blocks beside this one's are worth it where every SM has one tile at most (one token 5.2 us, and 5.6 where
     // they come at the end); beside many turns they only get in each other's way (quantisation and product, 8192 x 2048 x 2048: 29.4, and
     // 27.6 at the end).
@@ -652,47 +703,25 @@ int launch_form(const F4GemmArgs& a, Args g, int tile_rows, int box, int sms, cu
     return launch_status();
 }
 
-// Up to 32 rows: clusters of 2 or 4 CTAs share a tile's K where the tiles alone leave SMs idle.  (Quantisation and product, one row,
-// us without and with: K = N = 2048 6.9 and 6.3, 4096 10.0 and 7.7, 8192 15.6 and 12.2, K = 8192 N = 2048 15.2 and 8.8.  Clusters of 8
-// wait for so many free SMs of a GPC that they lose: 10.4 at 2048.  So does adding up 128 rows and more: 256 rows of 2048 8.2 and 11.5.)
-template <bool MX>
-int launch_few_rows(const F4GemmArgs& a, Args g, int sms, cudaStream_t st) {
-    const long long tiles = tiles_of(a, 32, BM);
-    const int box = a.M <= 16 ? 16 : 32;
-    g.split = 1;
-    while (g.split < MAX_SPLIT && tiles * g.split * 2 <= sms && g.split * 2 <= ceil_div(a.K, BK)) g.split *= 2;
-    return g.split > 1 ? launch_form<MX, false, 32, true>(a, g, 32, box, sms, st) : launch_form<MX, false, 32, false>(a, g, 32, box, sms, st);
-}
-
-// Which form.  Up to 32 rows: tiles of 32 (a group's second tile of 32 would start inside a tile of scales, so that these are 32
-// rows in all).  Else single CTAs (128 units x 128 rows), pairs of 256 units x 256 rows, or, without groups, of 192 rows (every second tile then
-// starts in the middle of a tile of scales), by the clocks that the SMs are estimated to take: the turns, what each takes as measured on
-// many turns (the epilogue's time where K is short), and the last one's epilogue.  Measured, us single / 192 / 256: 1024 rows, K = N =
-// 2048 6.8 / 8.0 / 8.1; 731 rows, N = 3307 11.1 / 9.0 / 9.4; 2048 rows 11.0 / 11.3 / 8.6; 4096 x 4096 x 4096 47.3 / 36.6 / 31.5; 4096 x 512 x
-// 4096 16.4 / 15.3 / 14.6; 16384 rows by 32 groups of 2048 x 4096 118 / 90 / 80.  (Pairs of 128 rows win nowhere.)
-// Groups of less than 128 rows on average are bound by their weights' bytes, and narrow tiles have more of them on their way: 2048
-// rows by 32 groups 19.3 and 21.2.
 template <bool MX>
 int launch_format(const F4GemmArgs& a, const Args& g, int sms, cudaStream_t st) {
-    if (a.M <= 32) return launch_few_rows<MX>(a, g, sms, st);
-    const int rows = a.offsets ? ceil_div(a.M, a.groups) : a.M;      // of a group, on average
-    const long long steps = ceil_div(a.K, BK);
-    auto clocks = [&](int tile, int ctas, long long shortest, long long step, long long more, long long last) {
-        // (half a tile for the rest of each group)
-        const long long row_tiles = a.offsets ? a.M / tile + (a.groups + 1) / 2 : ceil_div(a.M, tile);
-        const long long turns = (row_tiles * ceil_div(a.N, BM * ctas) + sms / ctas - 1) / (sms / ctas), turn = steps * step + more;
-        return turns * (turn > shortest ? turn : shortest) + last;
-    };
-    if (rows >= 128 && sms >= 2) {
-        const long long single = clocks(128, 1, 3500, 753, 1450, 1900), high = clocks(256, 2, 5200, 743, 2350, 3800);
-        const long long low = a.offsets ? high : clocks(192, 2, 3900, 700, 2200, 3000);
-        if (low < high && low < single) return launch_form<MX, true, PAIR_ROWS, false>(a, g, 192, 96, sms, st);
-        if (high < single) return launch_form<MX, true, PAIR_ROWS, false>(a, g, 256, 128, sms, st);
-    }
-    return launch_form<MX, false, 128, false>(a, g, 128, rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128, sms, st);
+    const Form f = form_of(sizes_of(a), sms);
+    if (f.ctas == 2) return launch_form<MX, true, PAIR_ROWS, false>(a, g, f, sms, st);
+    if (f.width == 128) return launch_form<MX, false, 128, false>(a, g, f, sms, st);
+    return f.split > 1 ? launch_form<MX, false, 32, true>(a, g, f, sms, st) : launch_form<MX, false, 32, false>(a, g, f, sms, st);
 }
 
 }  // namespace
+
+int f4_gemm_form(int M, int N, int K, int groups, int sms, bnn_f4_form* form) {
+    if (sms == 0) sms = device_sm_count();
+    if (sms < 1) return BNN_ERR_CUDA;
+    const Form f = form_of({M, N, K, groups}, sms);
+    form->ctas = f.ctas;
+    form->rows = f.tile_rows;
+    form->split = f.split;
+    return BNN_OK;
+}
 
 int launch_f4_gemm(const F4GemmArgs& a, cudaStream_t st) {
     const int sms = device_sm_count();
