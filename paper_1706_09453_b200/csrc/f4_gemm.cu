@@ -627,9 +627,11 @@ struct Sizes {
     int M, N, K, groups;
 };
 
-// An upper bound on the tiles of a form: the groups' rows are only known on the device.
+// An upper bound on the tiles of a form: the groups' rows are only known on the device.  n rows make at most (n + rows - 1) / rows tiles, and
+// at most min(M, groups) groups have any.  Of a dense matrix it is the number itself.
 long long tiles_of(const Sizes& z, int rows, int units) {
-    return (z.M / rows + (z.groups ? (long long)(z.M < z.groups ? z.M : z.groups) : 1)) * ceil_div(z.N, units);
+    const long long live = !z.groups ? 1 : z.M < z.groups ? z.M : z.groups;
+    return (z.M + live * (rows - 1)) / rows * ceil_div(z.N, units);
 }
 
 // How a product is cut up: tiles of ctas * 128 units x tile_rows rows (of `width` in the kernel's layout), copied `box` rows at a time, their K

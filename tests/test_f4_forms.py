@@ -27,3 +27,19 @@ def test_refusals(B):
     assert B.raw_call("bnn_f4_gemm_form", *good.values(), None) == 1
     for bad in (dict(M=0), dict(N=0), dict(K=0), dict(K=(1 << 24) + 1), dict(groups=-1), dict(groups=1025), dict(sms=-1), dict(M=0x7FFFFFFF), dict(N=0x7FFFFFFF)):
         assert B.raw_call("bnn_f4_gemm_form", *{**good, **bad}.values(), form) == 2, bad
+
+
+@pytest.mark.parametrize("N,K", [(2048, 2048), (4096, 4096), (8192, 8192), (2048, 8192), (1000, 700)])
+def test_no_step_at_thirty_two_rows(B, N, K):
+    """All of 17 to 32 rows are one tile, and share its K between as many CTAs."""
+    forms = {B.bnn_f4_gemm_form(M, N, K, 0, SMS) for M in range(17, 33)}
+    assert len(forms) == 1, forms
+    assert B.bnn_f4_gemm_form(32, N, K, 1, SMS) == B.bnn_f4_gemm_form(31, N, K, 1, SMS) in forms
+
+
+def test_few_rows_share_k_wherever_it_leaves_no_tile_waiting(B):
+    for N in range(128, 20000, 331):
+        tiles = -(-N // 128)
+        want = 4 if tiles * 4 <= SMS else 2 if tiles * 2 <= SMS else 1
+        for M in (1, 16, 31, 32):
+            assert B.bnn_f4_gemm_form(M, N, 4096, 0, SMS) == (1, 32, want), (M, N)
