@@ -242,3 +242,18 @@ def test_captured_on_pairs_beside_another_stream(env, fmt, M, N, K):
         for av, (a, asc, y, g, st) in zip(values, runs):
             assert torch.equal(y, exact_sums(av, wv).to(torch.bfloat16))
     assert B.bnn_device_status() == 0
+
+
+@pytest.mark.parametrize("M,N,K,form", [(20, 700, 2100, (1, 32, 4)), (9000, 2570, 1100, (2, 256, 1))])
+def test_offsets_that_make_no_sense_stay_inside(env, M, N, K, form):
+    torch, B = env
+    rng = np.random.default_rng(M)
+    for off in ([M, M // 2, 0, M], [-5, 10, 1 << 30, 3], [7, -1, 3, M + 40], [1 << 30] * 4, [0, M, 0, M]):
+        G = len(off) - 1
+        assert B.bnn_f4_gemm_form(M, N, K, G) == form
+        a, asc, _ = matrix(torch, rng, M, K, ref.MX, groups=G)
+        w, wsc, _ = matrix(torch, rng, G * N, K, ref.MX, np.arange(G + 1) * N, G)
+        y = torch.full((M + 1, N), 9.0, device=DEV)
+        B.bnn_f4_gemm_grouped(a, asc, torch.as_tensor(np.array(off, dtype=np.int64).astype(np.int32), device=DEV), w.view(G, N, -1), wsc, K, y[:M], ref.MX)
+        assert (y[M] == 9.0).all()
+    assert B.bnn_device_status() == 0
