@@ -511,7 +511,7 @@ BNN_API int bnn_pipe_rate(int which, int repeat, void* scratch, size_t scratch_b
  *            bnn_f4_scale_bytes(format, rows, K, groups) bytes.
  * Rows in groups (experts): offsets[0 .. groups] (DEVICE, ascending) -- group g has the rows
  * offsets[g] .. offsets[g+1]-1, and row tiles of its own, from tile offsets[g] / 128 + g on; a matrix without
- * offsets is one group.  Rows before the first and behind the last group are neither read nor written.  Offsets that
+ * offsets is one group.  Rows before the first and behind the last group are not written, and nothing depends on them.  Offsets that
  * do not ascend or leave the matrix give unspecified results, but no access outside the buffers.
  * groups <= 1024, K <= 2^24. */
 typedef enum { BNN_F4_E8M0_32 = 0, BNN_F4_E4M3_16 = 1 } bnn_f4_format;
@@ -521,7 +521,8 @@ BNN_API size_t bnn_f4_scale_bytes(int format, int rows, int K, int groups);
 
 /* Quantisation.  Row r of the result is row source[r] of X (source NULL: row r; an index outside
  * 0 .. src_rows-1 gives a row of zeros), times 2^exponent (|exponent| <= 64; e4m3 scales lose precision below 2^-6, which
- * is where weights of a fan-in of some thousands lie).  Scale of a block with largest magnitude m:
+ * is where weights of a fan-in of some thousands lie).  That product is one in fp32: what leaves its range is an infinity, what
+ * falls below its normal numbers is rounded.  Scale of a block with largest magnitude m:
  *   E8M0_32 : 2^(floor(log2 m) - 2), at least 2^-127;   E4M3_16 : m / 6 to the nearest e4m3 number, at most 448;
  * codes: x / scale to the nearest, ties to even, magnitudes above 6 become 6; zeros where the scale is 0.  A block with a NaN or an infinity
  * gets the scale NaN.  X : [src_rows][ldx] of `dtype`.
@@ -539,7 +540,7 @@ BNN_API int bnn_f4_dequantize(const void* codes, int ldc, const void* scales, si
 
 /* Product of two quantised matrices of one format, Eq. 1 with 4-bit weights and inputs:
  *   Y[m][n] = act(fma(2^exponent * scale[n], sum_k a[m][k] w[n][k], shift[n]))
- * with fp32 sums, whose order depends on the sizes.  A : [M] rows, W : [N] rows in the stored form above.  epi (may be NULL): scale, shift, and act
+ * with fp32 sums, whose order depends on the sizes and not on the row.  A : [M] rows, W : [N] rows in the stored form above.  epi (may be NULL): scale, shift, and act
  * BNN_ACT_NONE / HARDTANH / SIGMOID with Y [M][ldy] of `dtype`, or BNN_ACT_SIGN_PACK with Y NULL and out_bits (the input of a
  * binary layer).  Any M from one row on.
  * bnn_f4_gemm_grouped: group g's rows of A by W's rows g * N .. g * N + N - 1; W is [groups * N] rows whose scales are stored with
@@ -571,7 +572,7 @@ BNN_API int bnn_f4_gemm_form(int M, int N, int K, int groups, int sms, bnn_f4_fo
  *   offsets [E+1] : where each expert's pairs begin;   slot [T][k] : a pair's place;
  *   source [T*k]  : the token of the pair at a place -- what bnn_f4_quantize takes as `source`.
  * An expert with the logit -inf (or NaN) is not chosen.  Where fewer than k are left, index and slot are -1 and the
- * weight 0; places from offsets[E] on are not written.  A NaN makes all of its token's weights NaN, and so does +inf.
+ * weight 0; places from offsets[E] on are not written.  A NaN makes the weights of all of its token's choices NaN, and so does +inf.
  * E <= 1024, k <= 32, k <= E.  workspace: bnn_route_workspace_bytes(T, E) bytes, 16-byte aligned, not used
  * after the call's work is done.
  * Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN, BNN_ERR_UNSUPPORTED, BNN_ERR_WORKSPACE. */

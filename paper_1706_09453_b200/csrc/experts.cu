@@ -7,7 +7,12 @@
 // kOneBlock tokens one block does it all; beyond, a first kernel chooses and counts by block, and a second one adds the
 // counts of the blocks before (behind a kernel that sums them, where there are many) and places.  Bound by the instructions and the
 // latency of the picks, one maximum over the warp after the other: 16384 tokens, 256 experts, eight each, take 16.8 us in bf16 and 16.8 in
-// fp32, 5 of them the places (the logits' 8 or 17 MB are 1.3 or 2.6).  8 tokens, 64 experts: 3 us.
+// fp32, 5 of them the places (the logits' 8 or 17 MB are 1.3 or 2.6; one kernel at a time and from cold caches, as a profiler runs them, choice
+// and places take 16.0 and 9.6).  8 tokens, 64 experts: 3 us.  More than 512 experts are 32 logits a lane: the choice then keeps 56 to 64
+// bytes a thread in local memory.
+//
+// A weight is expf(logit - m) / sum in fp32.  Over the chosen experts the sum adds the same expf; over all of them it adds
+// 2^(x * log2 e) by the approximate instruction (fast_exp), a few 2^-22 of each term in no common direction.
 //
 // Weighted sum: bound by memory, 8192 tokens with four rows of 4096 bf16 each 53.5 us (6.3 TB/s).
 #include <cuda_bf16.h>
@@ -378,7 +383,7 @@ struct Plan {
 };
 Plan plan_of(int T) {
     if (T <= kOneBlock) return {kOneBlock, 1};
-    int chunk = ceil_div(T, 148);          // a block an SM, between a warp's worth of tokens and large masks
+    int chunk = ceil_div(T, f4::kSms);     // a block an SM, between a warp's worth of tokens and large masks
     chunk = chunk < 32 ? 32 : chunk > kMaxChunk ? kMaxChunk : chunk;
     return {chunk, ceil_div(T, chunk)};
 }
@@ -564,7 +569,7 @@ int launch_combine(const CombineArgs& a, cudaStream_t st) {
     const int zs = a.dtype == BNN_DTYPE_F32 ? 4 : 2, ys = a.y_dtype == BNN_DTYPE_F32 ? 4 : 2;
     const bool vec = a.N % 8 == 0 && aligned16(a.Z) && aligned16(a.Y) && ((long long)a.ldz * zs) % 16 == 0 && ((long long)a.ldy * ys) % 16 == 0;
     // Two pieces a lane where that leaves every SM a few blocks.
-    const int pieces = !vec ? 0 : a.N > SUM_THREADS * 8 && (long long)a.T * ceil_div(a.N, SUM_THREADS * 16) >= 148 * 8 ? 2 : 1;
+    const int pieces = !vec ? 0 : a.N > SUM_THREADS * 8 && (long long)a.T * ceil_div(a.N, SUM_THREADS * 16) >= f4::kSms * 8 ? 2 : 1;
     const int turns = ceil_div(a.N, SUM_THREADS * 8 * (pieces == 2 ? 2 : 1));
     if ((long long)a.T * turns > 0x7FFFFFFF) return BNN_ERR_SHAPE;
     void (*kern)(CombineArgs, int) = a.dtype == BNN_DTYPE_F32 ? combiner<float>(a.y_dtype, pieces)

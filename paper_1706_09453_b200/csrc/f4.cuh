@@ -13,6 +13,8 @@ namespace f4 {
 
 constexpr int kMaxGroups = 1024;
 constexpr int kMaxK = 1 << 24;
+// SMs that fixed thresholds and the plan of the router go by: the size of a workspace may not change with the current device.
+constexpr int kSms = 148;
 
 __host__ __device__ __forceinline__ int block_of(int format) { return format == BNN_F4_E8M0_32 ? 32 : 16; }
 // bytes of a row of codes

@@ -12,7 +12,8 @@
 //
 // Bound by the bytes that an SM takes in from L2: 42.5 a clock, which plain loads reach as well.  A step of a pair (256 units x 256
 // rows x 256 of K) is 36 KB, 843 clocks, for 512 of MMA; without any MMA 8192 x 4096 x 4096 takes 49.7 us instead of 52.9.  On top come
-// the stores (without them 97 us instead of 106 at 8192 x 4096 x 8192, 5.2 PFLOP/s) and, where K is short, the epilogue, 5200 clocks a
+// the stores (without them 97 us instead of 106 at 8192 x 4096 x 8192, 5.2 PFLOP/s; that is at the full clock, as replayed from a graph in short
+// runs: back to back under the power limit the same product takes 125 us, 4.4 PFLOP/s) and, where K is short, the epilogue, 5200 clocks a
 // tile.  Each TMA instruction costs as well: two copies of 64 rows and scale tiles one by one instead of one copy per operand were 118
 // us instead of 109.  e4m3 scales, of which there are twice as many, take 112.  Scale copies to tensor memory cost nothing measurable.
 #include <cuda_bf16.h>
@@ -641,7 +642,8 @@ struct Form {
 };
 
 // Up to 32 rows: clusters of 2 or 4 CTAs share a tile's K where the tiles alone leave SMs idle.  (Quantisation and product, one row,
-// us without and with: K = N = 2048 6.9 and 6.3, 4096 10.0 and 7.7, 8192 15.6 and 12.2, K = 8192 N = 2048 15.2 and 8.8.  Clusters of 8
+// us without and with: K = N = 2048 6.9 and 6.3, 4096 10.0 and 7.7, 8192 15.6 and 12.2, K = 8192 N = 2048 15.2 and 8.8; the product alone
+// on 31 or 32 rows: 5.5, 6.6, 11.9 and 7.6, and on 33, which do without: 5.8, 8.5, 14.5 and 13.8.  Clusters of 8
 // wait for so many free SMs of a GPC that they lose: 10.4 at 2048.  So does adding up 128 rows and more: 256 rows of 2048 8.2 and 11.5.)
 Form few_rows(const Sizes& z, int sms) {
     const long long tiles = tiles_of(z, 32, BM);

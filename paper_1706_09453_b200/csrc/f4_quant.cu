@@ -389,7 +389,7 @@ bool rows_aligned(const void* p, int dtype, int ld, int to) {
 // 1024 elements a warp where there is enough of that for every SM's warps (or too much for the grid's height), else 256.
 bool long_segments(int rows, int K) {
     const int segments = ceil_div(K, 256);
-    return segments > 65535 || ((long long)rows * segments >= 4LL * 148 * 64 && segments >= 4);
+    return segments > 65535 || ((long long)rows * segments >= 4LL * f4::kSms * 64 && segments >= 4);
 }
 // A warp's row and its columns are its block's coordinates (a division by the segments was a quarter of the instructions).
 dim3 grid_of(int rows, int K, int segment) { return dim3(ceil_div(rows, WARPS), ceil_div(K, segment)); }
