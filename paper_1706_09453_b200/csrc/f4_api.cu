@@ -48,7 +48,7 @@ int gemm_checked(const void* a, int lda, const void* a_scales, size_t a_scale_by
     if (exponent < -kMaxExponent || exponent > kMaxExponent) return BNN_ERR_SHAPE;
     if (int rc = check_groups(offsets, groups)) return rc;
     const long long units = (long long)groups * N;
-    if (units > 0x7FFFFFFF - 256 || M > 0x7FFFFFFF - 512) return BNN_ERR_SHAPE;
+    if (units > 0x7FFFFFFF - 256 || M > kMaxLength) return BNN_ERR_SHAPE;
     if (((long long)M / 32 + groups) * ceil_div(N, 128) > 0x7FFF0000) return BNN_ERR_SHAPE;
     if (int rc = check_f4(a, lda, a_scales, a_scale_bytes, format, M, groups, K)) return rc;
     if (int rc = check_f4(w, ldw, w_scales, w_scale_bytes, format, units, groups, K)) return rc;
@@ -176,7 +176,7 @@ int bnn_f4_gemm_grouped(const void* A, int lda, const void* a_scales, size_t a_s
 
 int bnn_f4_gemm_form(int M, int N, int K, int groups, int sms, bnn_f4_form* form) {
     if (!form) return BNN_ERR_NULL;
-    if (M < 1 || M > 0x7FFFFFFF - 512 || N < 1 || N > 0x7FFFFFFF - 256 || K < 1 || K > f4::kMaxK || groups < 0 || groups > f4::kMaxGroups || sms < 0)
+    if (M < 1 || M > kMaxLength || N < 1 || N > 0x7FFFFFFF - 256 || K < 1 || K > f4::kMaxK || groups < 0 || groups > f4::kMaxGroups || sms < 0)
         return BNN_ERR_SHAPE;
     return f4_gemm_form(M, N, K, groups, sms, form);
 }

@@ -22,6 +22,7 @@ def test_lengths_that_do_not_round_up(B, n):
             ("bnn_f4_quantize", abi.QUANTIZE, dict(rows=n, src_rows=n, K=32, scale_bytes=much)),
             ("bnn_f4_dequantize", abi.DEQUANTIZE, dict(rows=n, K=32, scale_bytes=much)),
             ("bnn_f4_gemm", abi.GEMM, dict(N=n, ldy=n, w_bytes=much)),
+            ("bnn_f4_gemm_grouped", abi.GROUPED, dict(M=n, N=1, K=32, ldy=1, groups=1024, a_bytes=much, w_bytes=much)),
             ("bnn_route_experts", abi.ROUTE, dict(T=n, E=1, k=1, bytes=much)),
             ("bnn_combine_experts", abi.COMBINE, dict(N=n, ldz=n, ldy=n)),
             ("bnn_combine_experts", abi.COMBINE, dict(N=n, ldz=n, ldy=n, z_dtype=2, y_dtype=2))):
