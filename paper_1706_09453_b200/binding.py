@@ -557,13 +557,13 @@ def _flat(t, dtype, n, what):
     return t.data_ptr()
 
 
-def _codes(t, k, width, dim=2):
-    """(address, pitch) of rows of codes, `width` bytes each.  Kernels take all bytes of a row that K elements need: of rows that are shorter (columns of
+def _codes(t, width, need, dim=2):
+    """(address, pitch) of rows of codes, `width` bytes each.  Kernels take all `need` bytes of a row, 16 for 32 elements: of rows that are shorter (columns of
     a wider tensor, say) the call is told the length instead, and refuses it."""
     stride = t.stride()
     if t.dtype is not torch.uint8 or len(stride) != dim or stride[-1] != 1:
         _refuse("codes: expected a %d-D uint8 tensor with contiguous rows" % dim)
-    return t.data_ptr(), stride[-2] if width >= (k + 31) // 32 * 16 else width
+    return t.data_ptr(), stride[-2] if width >= need else width
 
 
 def _scales(t):
@@ -595,7 +595,7 @@ def bnn_f4_quantize(X, codes, scales, fmt=F4_E8M0_32, source=None, offsets=None,
     _here((X, codes, scales, source, offsets))
     (rows, width), (src_rows, k) = codes.shape, X.shape
     src = 0 if source is None else _flat(source, torch.int32, rows, "source")
-    _f4_quantize(X.data_ptr(), _dtype(X), src_rows, k, _ld(X), src, *_groups(offsets), rows, fmt, exponent, *_codes(codes, k, width),
+    _f4_quantize(X.data_ptr(), _dtype(X), src_rows, k, _ld(X), src, *_groups(offsets), rows, fmt, exponent, *_codes(codes, width, k + 31 >> 5 << 4),
                  *_scales(scales), _stream())
     return codes, scales
 
@@ -606,14 +606,12 @@ def bnn_f4_dequantize(codes, scales, Y, fmt=F4_E8M0_32, offsets=None, exponent=0
     (rows, k), (n, width) = Y.shape, codes.shape
     if n != rows:
         _refuse("codes and Y have different numbers of rows")
-    _f4_dequantize(*_codes(codes, k, width), *_scales(scales), *_groups(offsets), rows, k, fmt, exponent, Y.data_ptr(), _dtype(Y), _ld(Y), _stream())
+    _f4_dequantize(*_codes(codes, width, k + 31 >> 5 << 4), *_scales(scales), *_groups(offsets), rows, k, fmt, exponent, Y.data_ptr(), _dtype(Y), _ld(Y), _stream())
     return Y
 
 
 def _f4_epilogue(rows, groups, n, act, sign_mode, scale, shift, out_bits):
-    """The epilogue of a product of n units a group; None where there is nothing to it."""
-    if act == ACT_NONE and scale is None and shift is None and out_bits is None:
-        return None
+    """The epilogue of a product of n units a group."""
     for t in (scale, shift):
         if t is not None:
             _flat(t, torch.float32, groups * n, "scale, shift")
@@ -635,9 +633,10 @@ def bnn_f4_gemm(A, a_scales, W, w_scales, K, Y=None, fmt=F4_E8M0_32, exponent=0,
                 out_bits=None, sign_mode=SIGN_ZERO_POS):
     """Y = act(fma(2^exponent * scale, A W^T, shift)) of two quantised matrices (codes uint8 [rows][pitch], scales)."""
     _here((A, a_scales, W, w_scales, Y, scale, shift, out_bits))
-    (m, a_width), (n, w_width) = A.shape, W.shape
-    e = _f4_epilogue(m, 1, n, act, sign_mode, scale, shift, out_bits)
-    _f4_gemm(*_codes(A, K, a_width), *_scales(a_scales), *_codes(W, K, w_width), *_scales(w_scales), m, n, K, fmt, exponent, *_f4_result(Y, m, n),
+    (m, a_width), (n, w_width), need = A.shape, W.shape, K + 31 >> 5 << 4
+    plain = act == ACT_NONE and scale is None and shift is None and out_bits is None
+    e = None if plain else _f4_epilogue(m, 1, n, act, sign_mode, scale, shift, out_bits)
+    _f4_gemm(*_codes(A, a_width, need), *_scales(a_scales), *_codes(W, w_width, need), *_scales(w_scales), m, n, K, fmt, exponent, *_f4_result(Y, m, n),
              0 if e is None else C.addressof(e), _stream())
     return Y if out_bits is None else out_bits
 
@@ -650,9 +649,10 @@ def bnn_f4_gemm_grouped(A, a_scales, offsets, W, w_scales, K, Y=None, fmt=F4_E8M
     shape, stride = W.shape, W.stride()
     if len(shape) != 3 or shape[0] != groups or (groups > 1 and stride[0] != shape[1] * stride[1]):
         _refuse("W: expected [%d, N, pitch], the groups one behind the other" % groups)
-    (m, a_width), (_, n, w_width) = A.shape, shape
-    e = _f4_epilogue(m, groups, n, act, sign_mode, scale, shift, out_bits)
-    _f4_gemm_grouped(*_codes(A, K, a_width), *_scales(a_scales), off, groups, *_codes(W, K, w_width, 3), *_scales(w_scales), m, n,
+    (m, a_width), (_, n, w_width), need = A.shape, shape, K + 31 >> 5 << 4
+    plain = act == ACT_NONE and scale is None and shift is None and out_bits is None
+    e = None if plain else _f4_epilogue(m, groups, n, act, sign_mode, scale, shift, out_bits)
+    _f4_gemm_grouped(*_codes(A, a_width, need), *_scales(a_scales), off, groups, *_codes(W, w_width, need, 3), *_scales(w_scales), m, n,
                      K, fmt, exponent, *_f4_result(Y, m, n), 0 if e is None else C.addressof(e), _stream())
     return Y if out_bits is None else out_bits
 
